@@ -18,6 +18,10 @@ EXPORTS = ["pi0_create", "pi0_destroy", "pi0_weights_bytes", "pi0_workspace_byte
            "pi0_set_graph_mode", "pi0_set_precision", "pi0_kernel_count", "pi0_strerror", "pi0_last_hip_error",
            "pi0_sync_dep_bench", "pi0_tune", "pi0_device_status", "pi0_loop_trace_ops", "pi0_set_loop_trace", "pi0_attention_probe"]
 
+# include/pi0_ops.h
+OPS_EXPORTS = ["pi0_pages_workspace_bytes", "pi0_pages_reserve", "pi0_pages_fork", "pi0_pages_compact", "pi0_pages_store", "pi0_pages_load",
+               "pi0_pages_status", "pi0_qk_norm_rope", "pi0_tree_attention_workspace_bytes", "pi0_tree_attention"]
+
 # enum pi0_op_class, in order
 OP_CLASSES = ["misc", "vis_patch", "vis_qkv", "vis_attn", "vis_o", "vis_up", "vis_down", "vis_proj", "reduce",
               "llm_qkv", "llm_attn", "llm_o", "llm_gateup", "llm_down", "exp_embed", "exp_qkv", "exp_attn", "exp_o",
@@ -37,6 +41,17 @@ class Pi0ConfigC(ctypes.Structure):
 def to_c_config(cfg) -> Pi0ConfigC:
     """Any object with the pi0_config field names (e.g. synth.Pi0Config) -> C struct."""
     return Pi0ConfigC(**{f: int(getattr(cfg, f)) for f in _FIELDS})
+
+
+class PagesC(ctypes.Structure):
+    _fields_ = ([(f, ctypes.c_void_p) for f in ("d_k", "d_v", "d_table", "d_length", "d_refs", "d_status")] +
+                [(f, ctypes.c_int64) for f in ("layer_stride", "page_stride", "token_stride", "head_stride")] +
+                [(f, ctypes.c_int32) for f in ("dtype", "layers", "n_pages", "page_tokens", "kv_heads", "head_dim", "n_seqs", "max_pages")])
+
+
+class RowsC(ctypes.Structure):
+    _fields_ = [("d_x", ctypes.c_void_p), ("row_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64), ("heads", ctypes.c_int32),
+                ("dtype", ctypes.c_int32)]
 
 
 _lib = None
@@ -108,16 +123,37 @@ def lib() -> ctypes.CDLL:
         L.pi0_strerror.restype = ctypes.c_char_p
         L.pi0_last_hip_error.argtypes = [vp]
         L.pi0_last_hip_error.restype = i32
+        pagesp, rowsp, f32 = ctypes.POINTER(PagesC), ctypes.POINTER(RowsC), ctypes.c_float
+        L.pi0_pages_workspace_bytes.argtypes = [pagesp]
+        L.pi0_pages_workspace_bytes.restype = sz
+        L.pi0_pages_reserve.argtypes = [pagesp, vp, vp, sz, vp]
+        L.pi0_pages_reserve.restype = i32
+        L.pi0_pages_fork.argtypes = [pagesp, vp, vp, i32, vp]
+        L.pi0_pages_fork.restype = i32
+        L.pi0_pages_compact.argtypes = [pagesp, vp, vp, i32, vp, vp, sz, vp]
+        L.pi0_pages_compact.restype = i32
+        L.pi0_pages_store.argtypes = [vp, pagesp, i32, vp]
+        L.pi0_pages_store.restype = i32
+        L.pi0_pages_load.argtypes = [vp, pagesp, i32, i32, vp]
+        L.pi0_pages_load.restype = i32
+        L.pi0_pages_status.argtypes = [pagesp, vp]
+        L.pi0_pages_status.restype = i32
+        L.pi0_qk_norm_rope.argtypes = [pagesp, i32, rowsp, rowsp, rowsp, rowsp, vp, i32, i32, vp, vp, vp, f32, f32, i32, ctypes.c_double, i32, vp]
+        L.pi0_qk_norm_rope.restype = i32
+        L.pi0_tree_attention_workspace_bytes.argtypes = [pagesp, i32, i32, i32]
+        L.pi0_tree_attention_workspace_bytes.restype = sz
+        L.pi0_tree_attention.argtypes = [pagesp, i32, rowsp, rowsp, vp, i32, i32, vp, i32, f32, vp, sz, vp]
+        L.pi0_tree_attention.restype = i32
         _lib = L
     return _lib
 
 
 class Pi0Error(RuntimeError):
-    def __init__(self, code: int, hip: int = 0):
+    def __init__(self, code: int, hip: int = 0, detail: str = ""):
         self.code = code
         self.hip = hip
         msg = lib().pi0_strerror(code).decode()
-        super().__init__(f"pi0 error {code}: {msg}" + (f" (hipError_t {hip})" if hip else ""))
+        super().__init__(f"pi0 error {code}: {msg}" + (f" (hipError_t {hip})" if hip else "") + (f": {detail}" if detail else ""))
 
 
 def pi0_weights_bytes(cfg) -> int:
@@ -335,3 +371,182 @@ class Pi0:
 
     def pi0_kernel_count(self, n_views: int, n_prompt: int) -> int:
         return int(lib().pi0_kernel_count(self._ctx, n_views, n_prompt))
+
+
+# ------------------------------------------------------------------ operators on a paged key/value cache (include/pi0_ops.h)
+_DTYPES = {"torch.bfloat16": 0, "torch.float16": 1, "torch.float32": 2}
+
+
+def _require(ok: bool, detail: str):
+    if not ok:
+        raise Pi0Error(PI0_EINVAL, detail=detail)
+
+
+def _int32(t, name: str, *shape):
+    """A contiguous int32 tensor of this shape (None: any size), as the library reads it."""
+    _require(str(t.dtype) == "torch.int32" and t.dim() == len(shape) and all(n is None or n == m for n, m in zip(shape, t.shape))
+             and t.is_contiguous(), f"{name}: contiguous int32 {list(shape)} expected")
+    return t
+
+
+class _On:
+    """For the length of a call: the device of a cache as the current one and `stream` (None: the device's default stream) as torch's,
+    so that scratch is allocated in the stream's order.  Tensors that belong to another stream than the call's stay allocated
+    until the call has run, also if the caller drops them."""
+
+    def __init__(self, pages, stream, tensors):
+        import torch
+        device = pages.device
+        self.stream = torch.cuda.default_stream(device) if stream is None else stream
+        _require(self.stream.device == device, "stream of another device")
+        self._enter = None
+        if torch.cuda.current_device() != device.index or torch.cuda.current_stream(device) != self.stream:
+            self._enter = torch.cuda.stream(self.stream)
+            for t in tensors:
+                if t is not None:
+                    t.record_stream(self.stream)
+            if self.stream not in pages._streams:
+                pages._streams.add(self.stream)
+                for t in (pages.k, pages.v, pages.table, pages.length, pages.refs, pages.status):
+                    t.record_stream(self.stream)
+        self.handle = int(self.stream.cuda_stream) or None
+
+    def __enter__(self):
+        if self._enter is not None:
+            self._enter.__enter__()
+        return self
+
+    def __exit__(self, *exc):
+        if self._enter is not None:
+            self._enter.__exit__(*exc)
+
+
+def _rows(t, name: str, n_rows: int, heads: Optional[int], head_dim: int, device) -> RowsC:
+    """[n_rows, heads, head_dim] with contiguous heads, any stride between rows and heads."""
+    _require(t.dim() == 3 and t.shape[0] == n_rows and (heads is None or t.shape[1] == heads) and t.shape[2] == head_dim and t.stride(2) == 1
+             and str(t.dtype) in _DTYPES and t.device == device, f"{name}: [{n_rows}, {heads or 'heads'}, {head_dim}] on {device} expected")
+    # (of a single row or head the stride says nothing)
+    row, head = t.stride(0) if n_rows > 1 else max(t.stride(0), head_dim), t.stride(1) if t.shape[1] > 1 else head_dim
+    return RowsC(t.data_ptr(), row, head, t.shape[1], _DTYPES[str(t.dtype)])
+
+
+class Pages:
+    """A paged key/value cache over the caller's tensors (struct pi0_pages), which stay the caller's:
+    k, v [layers, n_pages, page_tokens, kv_heads, head_dim] (bfloat16 or float16, one layout), table int32 [n_seqs, max_pages],
+    length int32 [n_seqs], refs int32 [n_pages].  An empty cache: table all -1, length and refs all 0."""
+
+    def __init__(self, k, v, table, length, refs):
+        import torch
+        _require(k.dim() == 5 and k.shape == v.shape and k.stride() == v.stride() and k.dtype == v.dtype and k.stride(4) == 1
+                 and str(k.dtype) in _DTYPES, "k, v: [layers, n_pages, page_tokens, kv_heads, head_dim] of one type and layout expected")
+        layers, n_pages, page_tokens, kv_heads, head_dim = k.shape
+        _int32(table, "table", None, None)
+        _int32(length, "length", table.shape[0])
+        _int32(refs, "refs", n_pages)
+        _require(k.is_cuda and all(t.device == k.device for t in (v, table, length, refs)), "all of a cache on one GPU expected")
+        self.k, self.v, self.table, self.length, self.refs = k, v, table, length, refs
+        self.device = k.device
+        self.status = torch.zeros(1, dtype=torch.int32, device=k.device)
+        torch.cuda.current_stream(k.device).synchronize()   # the word is 0 before a call on any stream looks at it
+        self._streams = set()   # other streams that calls have run on
+        self.n_seqs = int(table.shape[0])
+        self._c = PagesC(k.data_ptr(), v.data_ptr(), table.data_ptr(), length.data_ptr(), refs.data_ptr(), self.status.data_ptr(),
+                         *k.stride()[:4], _DTYPES[str(k.dtype)], layers, n_pages, page_tokens, kv_heads, head_dim, *table.shape)
+        self._ref = ctypes.byref(self._c)
+        self._plan_bytes = int(lib().pi0_pages_workspace_bytes(self._ref))
+        _require(self._plan_bytes > 0, "sizes or strides that the library does not take (struct pi0_pages)")
+
+    def _check(self, rc: int):
+        if rc != PI0_OK:
+            raise Pi0Error(rc)
+
+    def _scratch(self, nbytes: int):
+        import torch
+        return torch.empty(nbytes, dtype=torch.uint8, device=self.device)   # on the call's stream: its allocator keeps the order
+
+    def _on(self, stream, *tensors) -> _On:
+        _require(all(t is None or t.device == self.device for t in tensors), f"tensors on {self.device} expected")
+        return _On(self, stream, tensors)
+
+    def pi0_pages_reserve(self, extra, stream=None):
+        _int32(extra, "extra", self.n_seqs)
+        with self._on(stream, extra) as on:
+            ws = self._scratch(self._plan_bytes)
+            self._check(lib().pi0_pages_reserve(self._ref, _ptr(extra), _ptr(ws), self._plan_bytes, on.handle))
+
+    def pi0_pages_fork(self, src, dst, stream=None):
+        _int32(src, "src", None)
+        _int32(dst, "dst", src.shape[0])
+        with self._on(stream, src, dst) as on:
+            self._check(lib().pi0_pages_fork(self._ref, _ptr(src), _ptr(dst), src.shape[0], on.handle))
+
+    def pi0_pages_compact(self, keep, n_keep, start=None, stream=None):
+        """keep: int32 [n_seqs, keep_stride] or None; start: int32 [n_seqs] or None (the committed lengths)."""
+        _int32(n_keep, "n_keep", self.n_seqs)
+        if keep is not None:
+            _int32(keep, "keep", self.n_seqs, None)
+        if start is not None:
+            _int32(start, "start", self.n_seqs)
+        stride = 0 if keep is None else keep.shape[1]
+        with self._on(stream, keep, n_keep, start) as on:
+            ws = self._scratch(self._plan_bytes)
+            self._check(lib().pi0_pages_compact(self._ref, _ptr(start), _ptr(keep) if stride else None, stride, _ptr(n_keep), _ptr(ws),
+                                                self._plan_bytes, on.handle))
+
+    def pi0_pages_store(self, model: Pi0, seq: int, stream=None):
+        with self._on(stream) as on:
+            model._check(lib().pi0_pages_store(model._ctx, self._ref, int(seq), on.handle))
+
+    def pi0_pages_load(self, model: Pi0, seq: int, n_tokens: int, stream=None):
+        with self._on(stream) as on:
+            model._check(lib().pi0_pages_load(model._ctx, self._ref, int(seq), int(n_tokens), on.handle))
+
+    def pi0_pages_status(self, stream=None):
+        """Synchronises the stream; raises if an operation failed on the device since the last call."""
+        with self._on(stream) as on:
+            self._check(lib().pi0_pages_status(self._ref, on.handle))
+
+
+def pi0_qk_norm_rope(pages: Pages, layer: int, q, k, v, row_start, max_rows: int, *, out=None, positions=None, q_gain=None, k_gain=None,
+                     gain_offset: float = 1.0, eps: float = 1e-6, rope_dim: Optional[int] = None, rope_base: float = 10000.0,
+                     interleaved: bool = False, stream=None):
+    """q [n, heads, head_dim], k / v [n, kv_heads, head_dim]: norms, rotation, keys and values into the pages; returns the rotated
+    queries (`out`, or a new tensor).  rope_dim None: all of head_dim."""
+    import torch
+    c = pages._c
+    n, d = q.shape[0], c.head_dim
+    _int32(row_start, "row_start", pages.n_seqs + 1)
+    if positions is not None:
+        _int32(positions, "positions", n)
+    for g in (q_gain, k_gain):
+        _require(g is None or (str(g.dtype) == "torch.float32" and tuple(g.shape) == (d,) and g.is_contiguous()), f"gains: float32 [{d}] expected")
+    with pages._on(stream, q, k, v, out, row_start, positions, q_gain, k_gain) as on:
+        if out is None:
+            out = torch.empty(q.shape, dtype=pages.k.dtype, device=q.device)
+        rows = [_rows(t, *a, d, pages.device) for t, a in ((q, ("q", n, None)), (k, ("k", n, c.kv_heads)), (v, ("v", n, c.kv_heads)),
+                                                             (out, ("out", n, q.shape[1])))]
+        pages._check(lib().pi0_qk_norm_rope(pages._ref, int(layer), *[ctypes.byref(r) for r in rows], _ptr(row_start), n, int(max_rows),
+                                            _ptr(positions), _ptr(q_gain), _ptr(k_gain), float(gain_offset), float(eps),
+                                            d if rope_dim is None else int(rope_dim), float(rope_base), int(bool(interleaved)), on.handle))
+    return out
+
+
+def pi0_tree_attention(pages: Pages, layer: int, q, row_start, max_rows: int, *, mask=None, scale: Optional[float] = None, out=None, stream=None):
+    """q [n, heads, head_dim] of the cache's type; mask int32 [n, words] (bit j % 32 of word j / 32: sees token j of its sequence) or None
+    (all up to itself); scale None: head_dim ** -0.5.  Returns `out`, or a new tensor."""
+    import torch
+    n, d = q.shape[0], pages._c.head_dim
+    _int32(row_start, "row_start", pages.n_seqs + 1)
+    if mask is not None:
+        _int32(mask, "mask", n, None)
+    with pages._on(stream, q, out, row_start, mask) as on:
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        q_rows, o_rows = _rows(q, "q", n, None, d, pages.device), _rows(out, "out", n, q.shape[1], d, pages.device)
+        need = int(lib().pi0_tree_attention_workspace_bytes(pages._ref, q_rows.heads, n, int(max_rows)))
+        _require(need > 0, "heads, rows or max_rows that the library does not take")
+        ws = pages._scratch(need)
+        pages._check(lib().pi0_tree_attention(pages._ref, int(layer), ctypes.byref(q_rows), ctypes.byref(o_rows), _ptr(row_start), n,
+                                              int(max_rows), _ptr(mask), 0 if mask is None else mask.shape[1],
+                                              float(d ** -0.5 if scale is None else scale), _ptr(ws), need, on.handle))
+    return out

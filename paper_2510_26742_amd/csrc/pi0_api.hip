@@ -14,6 +14,7 @@
 #include "prefix_loop.h"
 #include "vision_loop.h"
 #include "pi0_internal.h"
+#include "pages_common.h"
 
 namespace {
 
@@ -2239,6 +2240,49 @@ int pi0_stream_frame(pi0_ctx* c, const float* d_images, int n_views, const int32
   c->cur_slot = nxt;
   c->cur_views = n_views;
   c->cur_prompt = n_prompt;
+  return PI0_OK;
+}
+
+// The two ways between the prefix that the ctx holds and a caller's pages (pages.hip), with pi0_prefill's rules about which
+// copy of the cache is written and who is told.
+static bool pages_take_prefix(const pi0_ctx* c, const pi0_pages* p, int seq) {
+  return pages_ok(p) && seq >= 0 && seq < p->n_seqs && p->kv_heads == 1 && p->head_dim == 256 && p->dtype == PI0_BF16 && p->layers == c->d.Ll;
+}
+// which prefix the ctx holds is known on the host: a call in a graph would go on with the one of its capture
+static hipError_t not_captured(hipStream_t s) {
+  hipStreamCaptureStatus capturing = hipStreamCaptureStatusNone;
+  const hipError_t e = s != nullptr ? hipStreamIsCapturing(s, &capturing) : hipSuccess;
+  return e == hipSuccess && capturing != hipStreamCaptureStatusNone ? hipErrorIllegalState : e;
+}
+
+int pi0_pages_store(pi0_ctx* c, const pi0_pages* pages, int seq, void* hip_stream) {
+  if (c == nullptr || !pages_take_prefix(c, pages, seq)) return PI0_EINVAL;
+  if (!c->loaded || c->cur_views == 0) return PI0_ESTATE;
+  const WsLayout& w = c->wl;
+  hipStream_t s = reinterpret_cast<hipStream_t>(hip_stream);
+  hipError_t e = not_captured(s);
+  if (e == hipSuccess)
+    e = launch_pages_store(s, *pages, seq, at<bf16>(c, w.kcache + c->cur_slot * w.kcache_slot), at<bf16>(c, w.vcache + c->cur_slot * w.vcache_slot),
+                           w.kcache_layer, w.vcache_layer, c->cur_views * c->d.T + c->cur_prompt);
+  return e == hipSuccess ? PI0_OK : fail_hip(c, e);
+}
+
+int pi0_pages_load(pi0_ctx* c, const pi0_pages* pages, int seq, int n_tokens, void* hip_stream) {
+  if (c == nullptr || !pages_take_prefix(c, pages, seq)) return PI0_EINVAL;
+  if (n_tokens < c->d.T || n_tokens > c->cfg.max_views * c->d.T + c->cfg.max_prompt) return PI0_EINVAL;
+  if (!c->loaded) return PI0_ESTATE;
+  const WsLayout& w = c->wl;
+  hipStream_t s = reinterpret_cast<hipStream_t>(hip_stream);
+  hipError_t e = not_captured(s);
+  if (e != hipSuccess) return fail_hip(c, e);
+  c->cur_views = 0;
+  e = launch_pages_load(s, *pages, seq, at<bf16>(c, w.kcache + c->cur_slot * w.kcache_slot), at<bf16>(c, w.vcache + c->cur_slot * w.vcache_slot),
+                                   w.kcache_layer, w.vcache_layer, n_tokens);
+  if (e == hipSuccess && c->ev_prefill[c->cur_slot] != nullptr) e = hipEventRecord(c->ev_prefill[c->cur_slot], s);
+  if (e != hipSuccess) return fail_hip(c, e);
+  // the denoise asks for their sum only (and graphs are kept by them): whole views, the rest as a prompt
+  c->cur_views = n_tokens / c->d.T;
+  c->cur_prompt = n_tokens - c->cur_views * c->d.T;
   return PI0_OK;
 }
 

@@ -1,0 +1,220 @@
+"""GPU: the operators together, as a program uses them - between a ctx's prefix and pages, and a step of drafting."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import paged
+from paper_2510_26742_amd import binding, synth
+
+pytestmark = pytest.mark.gpu
+DEV = torch.device("cuda:0")
+
+
+def ints(x):
+    return torch.tensor(np.asarray(x), dtype=torch.int32, device=DEV)
+
+
+def empty(layers, n_pages, page, n_seqs, max_pages, kv_heads=1, d=256, dtype=torch.bfloat16):
+    k, v = (torch.full((layers, n_pages, page, kv_heads, d), float("nan"), dtype=dtype, device=DEV) for _ in range(2))
+    return binding.Pages(k, v, ints(np.full((n_seqs, max_pages), -1)), ints([0] * n_seqs), ints([0] * n_pages))
+
+
+@pytest.fixture(scope="module")
+def model():
+    cfg = synth.reduced_config(vocab=512)
+    stream = torch.cuda.Stream()
+    m = binding.Pi0(cfg)
+    m.pi0_load_weights(torch.from_numpy(synth.make_weights(cfg, seed=0).view(np.int16)).to(DEV), stream)
+    stream.synchronize()
+    yield cfg, m, stream
+    m.close()
+
+
+def inputs(cfg, views, prompt, seed=0):
+    dev = lambda a: torch.from_numpy(a).to(DEV)
+    return (dev(synth.make_images(cfg, views, seed=21 + seed)), dev(synth.make_prompt(cfg, prompt, seed=24 + seed)) if prompt else None,
+            dev(synth.make_state(cfg, seed=22 + seed)), dev(synth.make_noise(cfg, seed=23 + seed)))
+
+
+def denoise(cfg, m, stream, state, noise):
+    out = torch.full((cfg.chunk, cfg.action_dim), float("nan"), device=DEV)
+    torch.cuda.synchronize()
+    m.pi0_denoise(state, noise, out, stream)
+    stream.synchronize()
+    return out
+
+
+@pytest.mark.parametrize("views,prompt,page", [(1, 0, 64), (1, 7, 16), (2, 21, 256), (3, 48, 32)])
+def test_prefix_through_pages_and_back(model, views, prompt, page):
+    """Prefill, store, another prefill in between, load: the denoise is the same, bit for bit; the pages hold the cache that
+    pi0_debug_forward reports."""
+    cfg, m, stream = model
+    P = views * 256 + prompt
+    images, ids, state, noise = inputs(cfg, views, prompt)
+    taps = torch.zeros(binding.pi0_debug_taps_elems(cfg, views, prompt), device=DEV)
+    out = torch.empty((cfg.chunk, cfg.action_dim), device=DEV)
+    m.pi0_debug_forward(images, views, ids, prompt, state, noise, out, taps, stream)
+    stream.synchronize()
+    at = cfg.vis_layers * views * 256 * cfg.vis_width + views * 256 * cfg.llm_width + (cfg.llm_layers - 1) * P * cfg.llm_width
+    want_k, want_v = taps[at:at + 2 * cfg.llm_layers * P * 256].view(2, cfg.llm_layers, P, 256)
+    m.pi0_prefill(images, views, ids, prompt, stream)
+    want = denoise(cfg, m, stream, state, noise)
+    pages = empty(cfg.llm_layers, 70, page, 3, 64)
+    pages.pi0_pages_reserve(ints([5, P, -1]), stream=stream)
+    pages.pi0_pages_store(m, 1, stream=stream)
+    pages.pi0_pages_status(stream)
+    assert pages.length.tolist() == [0, P, 0]
+    held = pages.table[1, :-(-P // page)].long()
+    for pool, ref in ((pages.k, want_k), (pages.v, want_v)):
+        assert torch.equal(pool[:, held].flatten(1, 3)[:, :P].float(), ref.to(torch.bfloat16).float())
+    # behind the last token, and in the other sequence's page, nothing is written
+    assert torch.isnan(pages.k[:, held].flatten(1, 3)[:, P:]).all() and torch.isnan(pages.v[:, pages.table[0, 0].long()]).all()
+    other = inputs(cfg, 1, 3, seed=9)
+    m.pi0_prefill(other[0], 1, other[1], 3, stream)
+    assert not torch.equal(denoise(cfg, m, stream, state, noise), want)
+    pages.pi0_pages_fork(ints([1]), ints([2]), stream=stream)
+    for seq in (1, 2):
+        pages.pi0_pages_load(m, seq, P, stream=stream)
+        assert torch.equal(denoise(cfg, m, stream, state, noise), want)
+    # into another ctx, too
+    m2 = binding.Pi0(cfg)
+    m2.pi0_load_weights(torch.from_numpy(synth.make_weights(cfg, seed=0).view(np.int16)).to(DEV), stream)
+    pages.pi0_pages_load(m2, 1, P, stream=stream)
+    assert torch.equal(denoise(cfg, m2, stream, state, noise), want)
+    # and what was loaded can be stored: the same rows in other pages
+    pages.pi0_pages_reserve(ints([P, -1, -1]), stream=stream)
+    pages.pi0_pages_store(m2, 0, stream=stream)
+    pages.pi0_pages_status(stream)
+    a, b = (pages.k[:, pages.table[s, :-(-P // page)].long()].flatten(1, 3)[:, :P] for s in (0, 1))
+    assert torch.equal(a, b)
+    m2.pi0_device_status(stream)
+    m2.close()
+
+
+@pytest.mark.parametrize("n", [256, 300, 337, 544, 700])
+def test_a_prefix_of_any_length_denoises_like_launches(model, n):
+    """Prefixes that no prefill leaves (tokens decoded behind it, or dropped): the persistent loop over them agrees with the
+    per-operation launches bit for bit."""
+    cfg, m, stream = model
+    images, ids, state, noise = inputs(cfg, 3, 48)
+    m.pi0_prefill(images, 3, ids, 48, stream)
+    pages = empty(cfg.llm_layers, 60, 16, 1, 60)
+    pages.pi0_pages_reserve(ints([816]), stream=stream)
+    pages.pi0_pages_store(m, 0, stream=stream)
+    keep = np.sort(np.random.default_rng(n).permutation(816)[:n])[None]
+    pages.pi0_pages_compact(ints(keep), ints([n]), start=ints([0]), stream=stream)
+    pages.pi0_pages_load(m, 0, n, stream=stream)
+    got = denoise(cfg, m, stream, state, noise)
+    static = torch.empty_like(got)
+    m.pi0_denoise_static(state, noise, static, stream)
+    stream.synchronize()
+    assert torch.isfinite(got).all() and torch.equal(got, static)
+    pages.pi0_pages_status(stream)
+    m.pi0_device_status(stream)
+
+
+def test_store_fails_without_own_pages_and_in_a_capture(model):
+    cfg, m, stream = model
+    images, ids, state, noise = inputs(cfg, 1, 0)
+    m.pi0_prefill(images, 1, None, 0, stream)
+    pages = empty(cfg.llm_layers, 12, 64, 3, 8)
+    for code, prepare in ((binding.PI0_ENOMEM, lambda: pages.pi0_pages_reserve(ints([255 - 64, -1, -1]), stream=stream)),
+                          (binding.PI0_EINVAL, lambda: (pages.pi0_pages_reserve(ints([256, -1, -1]), stream=stream),
+                                                        pages.pi0_pages_compact(ints([list(range(256))] * 3), ints([256, -1, -1]), stream=stream),
+                                                        pages.pi0_pages_fork(ints([0]), ints([1]), stream=stream)))):
+        prepare()
+        pages.pi0_pages_status(stream)
+        before = pages.length.tolist()
+        pages.pi0_pages_store(m, 0, stream=stream)
+        with pytest.raises(binding.Pi0Error) as e:
+            pages.pi0_pages_status(stream)
+        assert e.value.code == code and pages.length.tolist() == before and torch.isnan(pages.k).all()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        for call in (lambda: pages.pi0_pages_store(m, 2, stream=stream), lambda: pages.pi0_pages_load(m, 0, 256, stream=stream)):
+            with pytest.raises(binding.Pi0Error) as e:
+                call()
+            assert e.value.code == binding.PI0_EHIP
+    assert torch.isfinite(denoise(cfg, m, stream, state, noise)).all()      # the ctx still has its prefix
+
+
+@pytest.mark.parametrize("heads,kv_heads,d,page,dtype", [(8, 1, 256, 64, "bf16"), (12, 4, 64, 16, "f16")])
+def test_steps_of_drafting(heads, kv_heads, d, page, dtype):
+    """Several steps over two layers: room, norms and rotation into the cache, attention of the tree, some nodes accepted; one
+    sequence forked on the way.  Against the plain forms on what the cache holds, so a step's errors do not add up; the cache's
+    bookkeeping bit for bit throughout."""
+    t = {"bf16": torch.bfloat16, "f16": torch.float16}[dtype]
+    rng = np.random.default_rng(d)
+    n_seqs, layers = 4, 2
+    pages = empty(layers, 64, page, n_seqs, 12, kv_heads, d, t)
+    bits = lambda x: x.view(torch.int16).cpu().numpy().copy()
+    plain = paged.Cache(bits(pages.k), bits(pages.v), n_seqs, 12)
+    u = torch.finfo(t).eps / 2
+    f64 = lambda x: x.double().cpu().numpy()
+    gain = torch.from_numpy(0.1 * rng.standard_normal(d)).float().to(DEV)
+    for step, counts in enumerate([[40, 1, 17, 0], [1, 1, 1, 1], [9, 0, 5, 33], [7, 7, 7, 7], [1, 30, 2, 0]]):
+        print("[gpu] step", step, counts, flush=True)
+        if step == 2:
+            pages.pi0_pages_fork(ints([0]), ints([3]))
+            plain.fork([0], [3])
+        n, most = sum(counts), max(counts)
+        starts = np.concatenate([[0], np.cumsum(counts)])
+        pages.pi0_pages_reserve(ints(counts))
+        plain.reserve(counts)
+        sees = []
+        position = np.zeros(n, dtype=np.int64)
+        mask = np.zeros((n, -(-most // 32)), dtype=np.uint32)
+        for s, c in enumerate(counts):
+            x = np.zeros((c, c), dtype=bool)
+            for i in range(c):
+                if i:
+                    x[i] = x[int(rng.integers(i))]
+                x[i, i] = True
+                position[starts[s] + i] = plain.length[s] + x[i].sum() - 1
+                for j in np.flatnonzero(x[i]):
+                    mask[starts[s] + i, j // 32] |= np.uint32(1) << np.uint32(j % 32)
+            sees.append(x)
+        for layer in range(layers):
+            q, k, v = (torch.from_numpy(rng.standard_normal((n, h, d))).to(DEV, t) for h in (heads, kv_heads, kv_heads))
+            rotated = binding.pi0_qk_norm_rope(pages, layer, q, k, v, ints(starts), most, positions=ints(position), q_gain=gain, k_gain=gain)
+            out = binding.pi0_tree_attention(pages, layer, rotated, ints(starts), most, mask=ints(mask.view(np.int32)))
+            pages.pi0_pages_status()
+            for x, y in ((q, f64(rotated)),):
+                want = paged.norm_rope(f64(x), f64(gain), 1.0, 1e-6, position, d, 1e4, False)
+                assert (np.abs(y - want) <= u * np.abs(want) + 2.0 ** -18 * np.abs(want).max() + 2.0 ** -25).all()
+            want_k = paged.norm_rope(f64(k), f64(gain), 1.0, 1e-6, position, d, 1e4, False)
+            for s, c in enumerate(counts):
+                for i in range(c):
+                    a, b = plain.place(s, plain.length[s] + i)
+                    got = f64(pages.k[layer, a, b])
+                    r = starts[s] + i
+                    assert (np.abs(got - want_k[r]) <= u * np.abs(want_k[r]) + 2.0 ** -18 * np.abs(want_k[r]).max() + 2.0 ** -25).all()
+                    assert torch.equal(pages.v[layer, a, b], v[r])
+                    plain.k[layer, a, b], plain.v[layer, a, b] = bits(pages.k[layer, a, b]), bits(v[r])
+                if c == 0:
+                    continue
+                total = plain.length[s] + c
+                held = np.array(plain.table[s])[np.arange(total) // page], np.arange(total) % page
+                kk, vv = (f64(torch.from_numpy(pool[layer][held]).view(t)) for pool in (plain.k, plain.v))
+                see = np.concatenate([np.ones((c, plain.length[s]), dtype=bool), sees[s]], 1)
+                want = paged.attention(f64(rotated)[starts[s]:starts[s + 1]], kk, vv, see, d ** -0.5)
+                score = np.sqrt((f64(rotated) ** 2).sum(-1).max() * (kk ** 2).sum(-1).max()) * d ** -0.5
+                bar = (3 * u + 2.0 ** -24 * (2 * (d + 2) * score + 2 * total)) * np.abs(vv).max() + 2.0 ** -25
+                assert np.abs(f64(out)[starts[s]:starts[s + 1]] - want).max() <= bar
+        keep = np.zeros((n_seqs, most), dtype=np.int64)
+        n_keep = []
+        for s, c in enumerate(counts):
+            path = np.flatnonzero(sees[s][c - 1]) if c else np.zeros(0, dtype=int)      # the last node and its ancestors
+            if step == 0:
+                path = np.arange(c)
+            keep[s, :len(path)] = path
+            n_keep.append(len(path))
+        pages.pi0_pages_compact(ints(keep), ints(n_keep))
+        plain.compact(keep, n_keep)
+        pages.pi0_pages_status()
+        np.testing.assert_array_equal(pages.table.cpu().numpy(), plain.table_array())
+        np.testing.assert_array_equal(pages.length.cpu().numpy(), plain.length)
+        np.testing.assert_array_equal(pages.refs.cpu().numpy(), plain.refs)
+        np.testing.assert_array_equal(bits(pages.k), plain.k)
+        np.testing.assert_array_equal(bits(pages.v), plain.v)
+    assert plain.length[0] > 40
