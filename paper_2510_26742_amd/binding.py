@@ -6,6 +6,7 @@ fails loudly if the shared library has not been built.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from typing import Optional
@@ -374,60 +375,39 @@ class Pi0:
 
 
 # ------------------------------------------------------------------ operators on a paged key/value cache (include/pi0_ops.h)
-_DTYPES = {"torch.bfloat16": 0, "torch.float16": 1, "torch.float32": 2}
+# A call's work here is a few microseconds, which the smallest calls' kernels are not much longer than: no message is put
+# together before it is needed, and torch is asked once for what it knows.
+_types = {}      # torch type -> pi0_dtype
+_nothing = contextlib.nullcontext()
 
 
-def _require(ok: bool, detail: str):
-    if not ok:
-        raise Pi0Error(PI0_EINVAL, detail=detail)
+def _dtypes() -> dict:
+    if not _types:
+        import torch
+        _types.update({torch.bfloat16: 0, torch.float16: 1, torch.float32: 2, torch.int32: None})
+    return _types
+
+
+def _refuse(detail: str):
+    raise Pi0Error(PI0_EINVAL, detail=detail)
 
 
 def _int32(t, name: str, *shape):
     """A contiguous int32 tensor of this shape (None: any size), as the library reads it."""
-    _require(str(t.dtype) == "torch.int32" and t.dim() == len(shape) and all(n is None or n == m for n, m in zip(shape, t.shape))
-             and t.is_contiguous(), f"{name}: contiguous int32 {list(shape)} expected")
-    return t
+    if _dtypes().get(t.dtype, 0) is not None or t.dim() != len(shape) or not t.is_contiguous():
+        _refuse(f"{name}: contiguous int32 {list(shape)} expected")
+    for n, m in zip(shape, t.shape):
+        if n is not None and n != m:
+            _refuse(f"{name}: contiguous int32 {list(shape)} expected")
 
 
-class _On:
-    """For the length of a call: the device of a cache as the current one and `stream` (None: the device's default stream) as torch's,
-    so that scratch is allocated in the stream's order.  Tensors that belong to another stream than the call's stay allocated
-    until the call has run, also if the caller drops them."""
-
-    def __init__(self, pages, stream, tensors):
-        import torch
-        device = pages.device
-        self.stream = torch.cuda.default_stream(device) if stream is None else stream
-        _require(self.stream.device == device, "stream of another device")
-        self._enter = None
-        if torch.cuda.current_device() != device.index or torch.cuda.current_stream(device) != self.stream:
-            self._enter = torch.cuda.stream(self.stream)
-            for t in tensors:
-                if t is not None:
-                    t.record_stream(self.stream)
-            if self.stream not in pages._streams:
-                pages._streams.add(self.stream)
-                for t in (pages.k, pages.v, pages.table, pages.length, pages.refs, pages.status):
-                    t.record_stream(self.stream)
-        self.handle = int(self.stream.cuda_stream) or None
-
-    def __enter__(self):
-        if self._enter is not None:
-            self._enter.__enter__()
-        return self
-
-    def __exit__(self, *exc):
-        if self._enter is not None:
-            self._enter.__exit__(*exc)
-
-
-def _rows(t, name: str, n_rows: int, heads: Optional[int], head_dim: int, device) -> RowsC:
+def _rows(t, name: str, n_rows: int, heads: Optional[int], head_dim: int) -> RowsC:
     """[n_rows, heads, head_dim] with contiguous heads, any stride between rows and heads."""
-    _require(t.dim() == 3 and t.shape[0] == n_rows and (heads is None or t.shape[1] == heads) and t.shape[2] == head_dim and t.stride(2) == 1
-             and str(t.dtype) in _DTYPES and t.device == device, f"{name}: [{n_rows}, {heads or 'heads'}, {head_dim}] on {device} expected")
+    dtype, shape, stride = _dtypes().get(t.dtype), t.shape, t.stride()
+    if dtype is None or len(shape) != 3 or shape[0] != n_rows or heads not in (None, shape[1]) or shape[2] != head_dim or stride[2] != 1:
+        _refuse(f"{name}: [{n_rows}, {heads or 'heads'}, {head_dim}] of a floating type expected")
     # (of a single row or head the stride says nothing)
-    row, head = t.stride(0) if n_rows > 1 else max(t.stride(0), head_dim), t.stride(1) if t.shape[1] > 1 else head_dim
-    return RowsC(t.data_ptr(), row, head, t.shape[1], _DTYPES[str(t.dtype)])
+    return RowsC(t.data_ptr(), stride[0] if n_rows > 1 else max(stride[0], head_dim), stride[1] if shape[1] > 1 else head_dim, shape[1], dtype)
 
 
 class Pages:
@@ -437,48 +417,73 @@ class Pages:
 
     def __init__(self, k, v, table, length, refs):
         import torch
-        _require(k.dim() == 5 and k.shape == v.shape and k.stride() == v.stride() and k.dtype == v.dtype and k.stride(4) == 1
-                 and str(k.dtype) in _DTYPES, "k, v: [layers, n_pages, page_tokens, kv_heads, head_dim] of one type and layout expected")
+        if k.dim() != 5 or k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype or k.stride(4) != 1 or _dtypes().get(k.dtype) is None:
+            _refuse("k, v: [layers, n_pages, page_tokens, kv_heads, head_dim] of one type and layout expected")
         layers, n_pages, page_tokens, kv_heads, head_dim = k.shape
         _int32(table, "table", None, None)
         _int32(length, "length", table.shape[0])
         _int32(refs, "refs", n_pages)
-        _require(k.is_cuda and all(t.device == k.device for t in (v, table, length, refs)), "all of a cache on one GPU expected")
+        if not k.is_cuda or any(t.device != k.device for t in (v, table, length, refs)):
+            _refuse("all of a cache on one GPU expected")
         self.k, self.v, self.table, self.length, self.refs = k, v, table, length, refs
         self.device = k.device
         self.status = torch.zeros(1, dtype=torch.int32, device=k.device)
         torch.cuda.current_stream(k.device).synchronize()   # the word is 0 before a call on any stream looks at it
+        self._index = k.get_device()
         self._streams = set()   # other streams that calls have run on
         self.n_seqs = int(table.shape[0])
         self._c = PagesC(k.data_ptr(), v.data_ptr(), table.data_ptr(), length.data_ptr(), refs.data_ptr(), self.status.data_ptr(),
-                         *k.stride()[:4], _DTYPES[str(k.dtype)], layers, n_pages, page_tokens, kv_heads, head_dim, *table.shape)
+                         *k.stride()[:4], _dtypes()[k.dtype], layers, n_pages, page_tokens, kv_heads, head_dim, *table.shape)
         self._ref = ctypes.byref(self._c)
         self._plan_bytes = int(lib().pi0_pages_workspace_bytes(self._ref))
-        _require(self._plan_bytes > 0, "sizes or strides that the library does not take (struct pi0_pages)")
+        if self._plan_bytes == 0:
+            _refuse("sizes or strides that the library does not take (struct pi0_pages)")
 
     def _check(self, rc: int):
         if rc != PI0_OK:
             raise Pi0Error(rc)
 
+    def _on(self, stream, *tensors):
+        """(stream handle, context) of a call: inside the context the cache's device is the current one and the call's stream (None: the
+        device's default stream) torch's, so that scratch is allocated in the stream's order.  Tensors that belong to another
+        stream than the call's stay allocated until the call has run, also if the caller drops them."""
+        import torch
+        index = self._index
+        for t in tensors:
+            if t is not None and t.get_device() != index:
+                _refuse(f"tensors on {self.device} expected")
+        handle = 0 if stream is None else stream.cuda_stream
+        if stream is not None and stream.device_index != index:
+            _refuse(f"a stream of {self.device} expected")
+        if torch._C._cuda_getCurrentRawStream(index) == handle and torch._C._cuda_getDevice() == index:
+            return handle or None, _nothing
+        s = torch.cuda.default_stream(self.device) if stream is None else stream
+        for t in tensors:
+            if t is not None:
+                t.record_stream(s)
+        if handle not in self._streams:
+            self._streams.add(handle)
+            for t in (self.k, self.v, self.table, self.length, self.refs, self.status):
+                t.record_stream(s)
+        return handle or None, torch.cuda.stream(s)
+
     def _scratch(self, nbytes: int):
         import torch
-        return torch.empty(nbytes, dtype=torch.uint8, device=self.device)   # on the call's stream: its allocator keeps the order
-
-    def _on(self, stream, *tensors) -> _On:
-        _require(all(t is None or t.device == self.device for t in tensors), f"tensors on {self.device} expected")
-        return _On(self, stream, tensors)
+        return torch.empty(nbytes, dtype=torch.uint8, device=self.device)
 
     def pi0_pages_reserve(self, extra, stream=None):
         _int32(extra, "extra", self.n_seqs)
-        with self._on(stream, extra) as on:
+        handle, on = self._on(stream, extra)
+        with on:
             ws = self._scratch(self._plan_bytes)
-            self._check(lib().pi0_pages_reserve(self._ref, _ptr(extra), _ptr(ws), self._plan_bytes, on.handle))
+            self._check(lib().pi0_pages_reserve(self._ref, extra.data_ptr(), ws.data_ptr(), self._plan_bytes, handle))
 
     def pi0_pages_fork(self, src, dst, stream=None):
         _int32(src, "src", None)
         _int32(dst, "dst", src.shape[0])
-        with self._on(stream, src, dst) as on:
-            self._check(lib().pi0_pages_fork(self._ref, _ptr(src), _ptr(dst), src.shape[0], on.handle))
+        handle, on = self._on(stream, src, dst)
+        with on:
+            self._check(lib().pi0_pages_fork(self._ref, src.data_ptr(), dst.data_ptr(), src.shape[0], handle))
 
     def pi0_pages_compact(self, keep, n_keep, start=None, stream=None):
         """keep: int32 [n_seqs, keep_stride] or None; start: int32 [n_seqs] or None (the committed lengths)."""
@@ -488,23 +493,27 @@ class Pages:
         if start is not None:
             _int32(start, "start", self.n_seqs)
         stride = 0 if keep is None else keep.shape[1]
-        with self._on(stream, keep, n_keep, start) as on:
+        handle, on = self._on(stream, keep, n_keep, start)
+        with on:
             ws = self._scratch(self._plan_bytes)
-            self._check(lib().pi0_pages_compact(self._ref, _ptr(start), _ptr(keep) if stride else None, stride, _ptr(n_keep), _ptr(ws),
-                                                self._plan_bytes, on.handle))
+            self._check(lib().pi0_pages_compact(self._ref, _ptr(start), keep.data_ptr() if stride else None, stride, n_keep.data_ptr(), ws.data_ptr(),
+                                                self._plan_bytes, handle))
 
     def pi0_pages_store(self, model: Pi0, seq: int, stream=None):
-        with self._on(stream) as on:
-            model._check(lib().pi0_pages_store(model._ctx, self._ref, int(seq), on.handle))
+        handle, on = self._on(stream)
+        with on:
+            model._check(lib().pi0_pages_store(model._ctx, self._ref, int(seq), handle))
 
     def pi0_pages_load(self, model: Pi0, seq: int, n_tokens: int, stream=None):
-        with self._on(stream) as on:
-            model._check(lib().pi0_pages_load(model._ctx, self._ref, int(seq), int(n_tokens), on.handle))
+        handle, on = self._on(stream)
+        with on:
+            model._check(lib().pi0_pages_load(model._ctx, self._ref, int(seq), int(n_tokens), handle))
 
     def pi0_pages_status(self, stream=None):
         """Synchronises the stream; raises if an operation failed on the device since the last call."""
-        with self._on(stream) as on:
-            self._check(lib().pi0_pages_status(self._ref, on.handle))
+        handle, on = self._on(stream)
+        with on:
+            self._check(lib().pi0_pages_status(self._ref, handle))
 
 
 def pi0_qk_norm_rope(pages: Pages, layer: int, q, k, v, row_start, max_rows: int, *, out=None, positions=None, q_gain=None, k_gain=None,
@@ -514,20 +523,22 @@ def pi0_qk_norm_rope(pages: Pages, layer: int, q, k, v, row_start, max_rows: int
     queries (`out`, or a new tensor).  rope_dim None: all of head_dim."""
     import torch
     c = pages._c
-    n, d = q.shape[0], c.head_dim
+    n, d, kv_heads = q.shape[0], c.head_dim, c.kv_heads
     _int32(row_start, "row_start", pages.n_seqs + 1)
     if positions is not None:
         _int32(positions, "positions", n)
     for g in (q_gain, k_gain):
-        _require(g is None or (str(g.dtype) == "torch.float32" and tuple(g.shape) == (d,) and g.is_contiguous()), f"gains: float32 [{d}] expected")
-    with pages._on(stream, q, k, v, out, row_start, positions, q_gain, k_gain) as on:
+        if g is not None and (_dtypes().get(g.dtype) != 2 or g.shape != (d,) or not g.is_contiguous()):
+            _refuse(f"gains: float32 [{d}] expected")
+    handle, on = pages._on(stream, q, k, v, out, row_start, positions, q_gain, k_gain)
+    with on:
         if out is None:
-            out = torch.empty(q.shape, dtype=pages.k.dtype, device=q.device)
-        rows = [_rows(t, *a, d, pages.device) for t, a in ((q, ("q", n, None)), (k, ("k", n, c.kv_heads)), (v, ("v", n, c.kv_heads)),
-                                                             (out, ("out", n, q.shape[1])))]
-        pages._check(lib().pi0_qk_norm_rope(pages._ref, int(layer), *[ctypes.byref(r) for r in rows], _ptr(row_start), n, int(max_rows),
-                                            _ptr(positions), _ptr(q_gain), _ptr(k_gain), float(gain_offset), float(eps),
-                                            d if rope_dim is None else int(rope_dim), float(rope_base), int(bool(interleaved)), on.handle))
+            out = torch.empty(q.shape, dtype=pages.k.dtype, device=pages.device)
+        q_rows, k_rows = _rows(q, "q", n, None, d), _rows(k, "k", n, kv_heads, d)
+        v_rows, o_rows = _rows(v, "v", n, kv_heads, d), _rows(out, "out", n, q_rows.heads, d)
+        pages._check(lib().pi0_qk_norm_rope(pages._ref, layer, ctypes.byref(q_rows), ctypes.byref(k_rows), ctypes.byref(v_rows),
+                                            ctypes.byref(o_rows), row_start.data_ptr(), n, max_rows, _ptr(positions), _ptr(q_gain), _ptr(k_gain),
+                                            gain_offset, eps, d if rope_dim is None else rope_dim, rope_base, 1 if interleaved else 0, handle))
     return out
 
 
@@ -539,14 +550,17 @@ def pi0_tree_attention(pages: Pages, layer: int, q, row_start, max_rows: int, *,
     _int32(row_start, "row_start", pages.n_seqs + 1)
     if mask is not None:
         _int32(mask, "mask", n, None)
-    with pages._on(stream, q, out, row_start, mask) as on:
+    handle, on = pages._on(stream, q, out, row_start, mask)
+    with on:
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        q_rows, o_rows = _rows(q, "q", n, None, d, pages.device), _rows(out, "out", n, q.shape[1], d, pages.device)
-        need = int(lib().pi0_tree_attention_workspace_bytes(pages._ref, q_rows.heads, n, int(max_rows)))
-        _require(need > 0, "heads, rows or max_rows that the library does not take")
+            out = torch.empty(q.shape, dtype=q.dtype, device=pages.device)
+        q_rows = _rows(q, "q", n, None, d)
+        o_rows = _rows(out, "out", n, q_rows.heads, d)
+        need = lib().pi0_tree_attention_workspace_bytes(pages._ref, q_rows.heads, n, max_rows)
+        if need == 0:
+            _refuse("heads, rows or max_rows that the library does not take")
         ws = pages._scratch(need)
-        pages._check(lib().pi0_tree_attention(pages._ref, int(layer), ctypes.byref(q_rows), ctypes.byref(o_rows), _ptr(row_start), n,
-                                              int(max_rows), _ptr(mask), 0 if mask is None else mask.shape[1],
-                                              float(d ** -0.5 if scale is None else scale), _ptr(ws), need, on.handle))
+        pages._check(lib().pi0_tree_attention(pages._ref, layer, ctypes.byref(q_rows), ctypes.byref(o_rows), row_start.data_ptr(), n, max_rows,
+                                              _ptr(mask), 0 if mask is None else mask.shape[1], d ** -0.5 if scale is None else scale,
+                                              ws.data_ptr(), need, handle))
     return out
