@@ -15,6 +15,7 @@
 
 namespace {
 
+typedef f16 f16x2 __attribute__((ext_vector_type(2)));
 typedef f16 f16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
@@ -43,253 +44,494 @@ struct TreeArgs {
   const void* q;
   void* out;
   int64_t q_row_stride, q_head_stride, out_row_stride, out_head_stride;
-  int heads, group;      // query heads per key/value head
+  int group;             // query heads per key/value head
   const int* row_start;
   int n_rows, max_rows;
   const unsigned* mask;
   int mask_words;
-  float scale;           // times log2(e)
-  int row_tiles;         // of a sequence and key/value head, at most
+  float scale;           // times log2(e), >= 0
+  short negate;          // 0x8000 where the queries' signs are turned instead of the scale's
+  short zero;            // queries are all zero (scale 0)
+  int near_rows;         // eight rows of a page lie within 32 bits of offsets
   int64_t layer;         // elements in front of the layer
+  // workspace
+  int64_t* prefix;       // [n_seqs + 1] granules in front of a sequence, [n_seqs + 1] granules per block
+  float* part_o;         // [blocks][2][rows of a tile][head_dim]
+  float2* part_ml;       // [blocks][2][rows of a tile]
 };
 
-// The wave's 32 rows of queries and their running state.  C layout of a 32x32 product: lane = column (row of queries)
-// + 32 h, register i = row 8 (i / 4) + 4 h + i % 4.
+// How the work is cut.  A unit is 32 RW rows of one sequence and key/value head against all of its keys, in granules of 32 KW keys.
+// The granules of all units, in the order (sequence, head, row tile, granule), are dealt out to the blocks in equal runs: lengths differ,
+// and the host does not know them.  A block writes a unit that lies in its run as a whole; of the unit that its run begins inside of
+// it leaves a partial result in slot 0, of the one that goes on behind its run in slot 1, for the second launch.
+template <int D, int RW>
+struct Shape;
+// K and V tiles of a stage are KW x 64 D x 2 bytes; STAGES of them fill 128 KB where a row tile is 32 rows (bytes in
+// flight are what the speed is made of there)
+template <> struct Shape<256, 1> { static constexpr int KW = 2, STAGES = 2, BLOCKS = 256; };
+template <> struct Shape<128, 1> { static constexpr int KW = 4, STAGES = 2, BLOCKS = 256; };
+template <> struct Shape<64, 1> { static constexpr int KW = 4, STAGES = 4, BLOCKS = 256; };
+template <> struct Shape<256, 4> { static constexpr int KW = 1, STAGES = 4, BLOCKS = 256; };
+template <> struct Shape<128, 4> { static constexpr int KW = 1, STAGES = 4, BLOCKS = 512; };
+template <> struct Shape<64, 4> { static constexpr int KW = 1, STAGES = 4, BLOCKS = 512; };
+
+// page_at for a sequence and entry that are the same for the whole wave: through the scalar cache, so that it does not
+// wait in line behind the tiles that are on their way
+__device__ __forceinline__ int uniform_page(const pi0_pages& p, int seq, int idx) {
+  if (idx >= p.max_pages) return -1;
+  const int page = ((const __attribute__((address_space(4))) int*)p.d_table)[(size_t)seq * p.max_pages + idx];
+  return page >= 0 && page < p.n_pages ? page : -1;
+}
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
+// Reads of tiles by LDS address.  A tile's rows are 2 D bytes, its pieces permuted by an exclusive or with the key, so the address
+// of piece c is that of piece 0 of the same lane with bits turned over.
+typedef const __attribute__((address_space(3))) s16x8* LdsPiece;
+typedef __attribute__((address_space(3))) s16x4* LdsQuad;
+
+// S^T has a lane own one row of queries: lane = column (row of queries) + 32 h, register i = key 8 (i / 4) + 4 h + i % 4; O^T the
+// same with d in the place of keys.
 template <int D>
 struct RowState {
   f32x16 o[D / 32];
-  float m, l;
+  float m, l;   // reference of the exponents, sum of this lane's weights
 };
 
+__device__ __forceinline__ float dot_ones(bf16x2 w, float c) { return __builtin_amdgcn_fdot2_f32_bf16(w, bf16x2{(bf16)1.0f, (bf16)1.0f}, c, false); }
+__device__ __forceinline__ float dot_ones(f16x2 w, float c) { return __builtin_amdgcn_fdot2(w, f16x2{(f16)1.0f, (f16)1.0f}, c, false); }
+
+// whether 16 bytes of LDS hold an infinity or a NaN; CLEAN: puts zeros in their place
+template <class T, bool CLEAN>
+__device__ __forceinline__ bool clean(unsigned char* at) {
+  constexpr unsigned E = Mat<T>::EXPONENT;
+  uint4 u = *reinterpret_cast<const uint4*>(at);
+  unsigned word[4] = {u.x, u.y, u.z, u.w};
+  bool odd = false;
+#pragma unroll
+  for (int i = 0; i < 4; i++) {
+    const bool lo = (word[i] & E) == E, hi = (word[i] >> 16 & E) == E;
+    odd |= lo || hi;
+    word[i] &= (lo ? 0xffff0000u : ~0u) & (hi ? 0x0000ffffu : ~0u);
+  }
+  if (CLEAN && odd) *reinterpret_cast<uint4*>(at) = uint4{word[0], word[1], word[2], word[3]};
+  return odd;
+}
+
 // T: type; RW waves side by side have 32 rows each, KW of those groups a tile of 32 keys each
-template <class T, int D, int RW, int KW>
-__global__ __launch_bounds__(64 * RW * KW) void tree_attention_kernel(TreeArgs a) {
-  constexpr int PIECES = D / 8, TILE = 32 * D * 2, REQUESTS = TILE / 1024, KEYS_PER_REQUEST = 512 / D;
-  constexpr int ROWS = 32 * RW, WAVES = RW * KW;
+template <class T, int D, int RW>
+__global__ __launch_bounds__((64 * RW * Shape<D, RW>::KW)) void tree_attention_kernel(TreeArgs a) {
+  constexpr int KW = Shape<D, RW>::KW, STAGES = Shape<D, RW>::STAGES, WAVES = RW * KW, THREADS = 64 * WAVES;
+  constexpr int PIECES = D / 8, TILE = 32 * D * 2, REQUESTS = TILE / 1024 / RW, KEYS_PER_REQUEST = 512 / D;
+  constexpr int ROWS = 32 * RW, KEYS = 32 * KW;
+  static_assert(REQUESTS >= 1 && STAGES >= 2 && (STAGES - 2) * 2 * REQUESTS < 64, "the wait counter holds what is in flight");
+  typedef T T2 __attribute__((ext_vector_type(2)));
+  typedef T T4 __attribute__((ext_vector_type(4)));
   const pi0_pages& p = a.p;
-  __shared__ __align__(1024) unsigned char tiles[2][KW][TILE];
-  unsigned char (*const lds_k)[TILE] = tiles[0];
-  unsigned char (*const lds_v)[TILE] = tiles[1];
-  __shared__ float weights[WAVES][32][33];
+  __shared__ __align__(1024) unsigned char tiles[STAGES][2][KW][TILE];
+  __shared__ int64_t prefix[1025];
+  __shared__ int64_t sums[WAVES];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int rw = wave % RW, kw = wave / RW, h = lane >> 5;
 
-  const int unit = blockIdx.x;
-  const int tile_of_rows = unit % a.row_tiles, kv_head = unit / a.row_tiles % p.kv_heads, seq = unit / a.row_tiles / p.kv_heads;
-  const int2 rows = rows_of(a.row_start, seq, a.n_rows, a.max_rows);
-  if (tile_of_rows * ROWS >= rows.y * a.group) return;
-  const int length = length_of(p, seq), total = min(length + rows.y, p.max_pages * p.page_tokens);
-
-  // this lane's row: token and head
-  const int r = tile_of_rows * ROWS + rw * 32 + (lane & 31);
-  const bool live = r < rows.y * a.group;
-  const int node = live ? r / a.group : 0, head = kv_head * a.group + (live ? r % a.group : 0);
-  s16x8 q[D / 16];
-#pragma unroll
-  for (int i = 0; i < D / 16; i++) {
-    q[i] = s16x8{};
-    if (live)
-      q[i] = *reinterpret_cast<const s16x8*>(reinterpret_cast<const T*>(a.q) + (rows.x + node) * a.q_row_stride + head * a.q_head_stride + i * 16 + h * 8);
-  }
-  const unsigned* mask = a.mask != nullptr ? a.mask + (size_t)(rows.x + node) * a.mask_words : nullptr;
-
-  RowState<D> st;
-#pragma unroll
-  for (int b = 0; b < D / 32; b++) st.o[b] = f32x16{};
-  st.m = -INFINITY;
-  st.l = 0.f;
-
-  const int fk_key = lane & 31;
-  const int swz_k = (D == 64 ? (fk_key >> 1) & 7 : fk_key & 15) ^ h;
-  const int vkey = (lane & 15) >> 2;   // key of a group of four that this lane names in a transposing load
-  const int swz_v = D == 64 ? (vkey >> 1) & 1 : vkey;
-  const char* const pool_k = reinterpret_cast<const char*>(p.d_k) + 2 * (a.layer + kv_head * p.head_stride);
-  const char* const pool_v = reinterpret_cast<const char*>(p.d_v) + 2 * (a.layer + kv_head * p.head_stride);
-  const int shift = 31 - __clz(p.page_tokens);
-
-  for (int base = 0; base < total; base += 32 * KW) {
-    const int pos0 = base + kw * 32;
-    const int page0 = page_at(p, seq, pos0 >> shift), page1 = page_at(p, seq, (pos0 + 16) >> shift);
-    __syncthreads();   // the tiles of the round before have been read
-#pragma unroll
-    for (int j = 0; j < (REQUESTS + RW - 1) / RW; j++) {
-      const int request = j * RW + rw;
-      if (REQUESTS % RW != 0 && request >= REQUESTS) break;
-      const int key = request * KEYS_PER_REQUEST + lane / PIECES, pos = pos0 + key;
-      const int page = key < 16 ? page0 : page1;
-      const bool there = pos < total && page >= 0;
-      const int64_t at = 2 * (page * p.page_stride + (pos & (p.page_tokens - 1)) * p.token_stride);
-      const int piece = lane % PIECES;
-      const int piece_k = piece ^ (D == 64 ? (key >> 1) & 7 : key & 15);
-      const int piece_v = piece ^ (D == 64 ? ((key >> 1) & 1) << 2 : (key & 3) << 2);
-      const char* from_k = there ? pool_k + at + piece_k * 16 : reinterpret_cast<const char*>(zero_piece);
-      const char* from_v = there ? pool_v + at + piece_v * 16 : reinterpret_cast<const char*>(zero_piece);
-      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_address(lds_k[kw]) + request * 1024), "v"(from_k) : "memory");
-      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_address(lds_v[kw]) + request * 1024), "v"(from_v) : "memory");
+  // granules in front of each sequence
+  {
+    const int per_thread = div_up(p.n_seqs, THREADS), s0 = threadIdx.x * per_thread;
+    int64_t mine = 0;
+    for (int s = s0; s < min(p.n_seqs, s0 + per_thread); s++) {
+      const int n = rows_of(a.row_start, s, a.n_rows, a.max_rows).y;
+      const int total = min(length_of(p, s) + n, p.max_pages * p.page_tokens);
+      prefix[s + 1] = (int64_t)p.kv_heads * div_up(n * a.group, ROWS) * div_up(total, KEYS);
+      mine += prefix[s + 1];
     }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    int64_t upto = mine;
+    for (int i = 1; i < 64; i <<= 1) {
+      const int64_t u = __shfl_up(upto, i);
+      if (lane >= i) upto += u;
+    }
+    if (lane == 63) sums[wave] = upto;
     __syncthreads();
+    for (int w = 0; w < wave; w++) upto += sums[w];
+    int64_t before = upto - mine;
+    if (threadIdx.x == 0) prefix[0] = 0;
+    for (int s = s0; s < min(p.n_seqs, s0 + per_thread); s++) {
+      before += prefix[s + 1];
+      prefix[s + 1] = before;
+    }
+    __syncthreads();
+  }
+  const int64_t all = prefix[p.n_seqs], run = max((int64_t)1, (all + gridDim.x - 1) / gridDim.x);
+  if (blockIdx.x == 0) {
+    for (int s = threadIdx.x; s <= p.n_seqs; s += THREADS) a.prefix[s] = prefix[s];
+    if (threadIdx.x == 0) a.prefix[p.n_seqs + 1] = run;
+  }
+  const int64_t begin = blockIdx.x * run, end = min(all, begin + run);
 
-    // S^T
-    f32x16 s = {};
-    const unsigned char* kt = lds_k[kw] + fk_key * (2 * D);
+  // This lane's pieces.  First product: key lane % 32, pieces h, h + 2, ..; second: of 4 keys and 16 d that 16 lanes read transposed,
+  // key (lane % 16) / 4 and quad lane % 4.  Requests: row lane / PIECES of a KiB, its piece lane % PIECES - where the row's
+  // permuted piece lies in the cache.
+  const int kkey = lane & 31, vkey = (lane & 15) >> 2;
+  const unsigned read_k = kkey * 2 * D + (((D == 64 ? (kkey >> 1) & 7 : kkey & 15) ^ h) << 4);
+  const unsigned read_v = (4 * h + vkey) * 2 * D + ((D == 64 ? (vkey >> 1) & 1 : vkey) << 6) + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
+  const int my_row = lane / PIECES, my_piece = lane % PIECES;
+  const int piece_k0 = my_piece ^ (D == 64 ? (my_row >> 1) & 7 : my_row), piece_v0 = my_piece ^ (D == 64 ? ((my_row >> 1) & 1) << 2 : (my_row & 3) << 2);
+  const int shift = 31 - __clz(p.page_tokens), in_page = p.page_tokens - 1;
+  const unsigned lds0 = lds_address(&tiles[0][0][0][0]);
+
+  for (int64_t cur = begin; cur < end;) {
+    // the unit that this run is in
+    int seq = 0;
+    for (int top = p.n_seqs; top - seq > 1;) {
+      const int mid = (seq + top) >> 1;
+      if (prefix[mid] <= cur) seq = mid;
+      else top = mid;
+    }
+    seq = uniform(seq);
+    const int2 rows = rows_of(a.row_start, seq, a.n_rows, a.max_rows);
+    const int length = uniform(length_of(p, seq)), total = uniform(min(length + rows.y, p.max_pages * p.page_tokens));
+    const int granules = div_up(total, KEYS), row_tiles = uniform(div_up(rows.y * a.group, ROWS));
+    const int64_t inside = cur - prefix[seq];
+    const int unit = uniform((int)(inside / granules)), g0 = uniform((int)(inside - (int64_t)unit * granules));
+    const int g1 = uniform((int)min((int64_t)granules, g0 + (end - cur)));
+    const int kv_head = unit / row_tiles, row_tile = unit - kv_head * row_tiles;
+    cur += g1 - g0;
+
+    // this lane's row: token and head
+    const int r = row_tile * ROWS + rw * 32 + (lane & 31);
+    const bool live = r < rows.y * a.group;
+    const int node = live ? r / a.group : 0, head = kv_head * a.group + (live ? r - node * a.group : 0);
+    s16x8 q[D / 16];
 #pragma unroll
     for (int i = 0; i < D / 16; i++) {
-      const s16x8 kf = *reinterpret_cast<const s16x8*>(kt + ((swz_k ^ (2 * i)) << 4));
-      s = Mat<T>::mfma(kf, q[i], s);
+      q[i] = s16x8{};
+      if (live && !a.zero)
+        q[i] = *reinterpret_cast<const s16x8*>(reinterpret_cast<const T*>(a.q) + (rows.x + node) * a.q_row_stride + head * a.q_head_stride + i * 16 + h * 8) ^ a.negate;
     }
-    // what of the tile the row sees, a bit per key
-    unsigned seen = 0xffffffffu;
-    const bool drafts = pos0 + 32 > length;
-    if (drafts || page0 < 0 || page1 < 0) {
-      const int j0 = pos0 - length;   // node at the tile's first key
-      if (drafts) {
-        unsigned nodes = 0;           // bit b: node max(j0, 0) + b
-        const int jn = max(j0, 0);
-        if (mask != nullptr) {
-          const int word = jn >> 5, off = jn & 31;
-          const unsigned lo = word < a.mask_words ? mask[word] : 0, hi = word + 1 < a.mask_words ? mask[word + 1] : 0;
-          nodes = (unsigned)(((unsigned long long)hi << 32 | lo) >> off);
+    const unsigned* mask = a.mask != nullptr ? a.mask + (size_t)(rows.x + node) * a.mask_words : nullptr;
+    const char* const pool_k = reinterpret_cast<const char*>(p.d_k) + 2 * (a.layer + kv_head * p.head_stride);
+    const char* const pool_v = reinterpret_cast<const char*>(p.d_v) + 2 * (a.layer + kv_head * p.head_stride);
+
+    // Requests this wave's part of a granule, of whose keys the first and last 16 lie in pages page0 and page1 (-1: none; a granule
+    // behind the last is asked for as well, as zeros, so that as many requests are in flight at the end as anywhere).
+    auto request = [&](int granule, int stage, int page0, int page1) {
+      const int pos0 = granule * KEYS + kw * 32;
+      const unsigned to = lds0 + ((stage * 2) * KW + kw) * TILE;
+      const bool whole = pos0 + 32 <= total && page0 >= 0 && page1 >= 0 && a.near_rows;
+#pragma unroll
+      for (int j = 0; j < REQUESTS; j++) {
+        const int part = j * RW + rw, key0 = part * KEYS_PER_REQUEST;   // the KiB and its first key
+        const int page = key0 < 16 ? page0 : page1;
+        const unsigned to_k = to + part * 1024, to_v = to_k + KW * TILE;
+        const int piece_k = piece_k0 ^ (D == 64 ? (key0 >> 1) & 7 : key0 & 15), piece_v = piece_v0 ^ (D == 64 ? ((key0 >> 1) & 1) << 2 : (key0 & 3) << 2);
+        if (whole) {
+          const int64_t at = 2 * (page * p.page_stride + ((pos0 + key0) & in_page) * p.token_stride);
+          const unsigned off = my_row * (unsigned)(2 * p.token_stride);
+          request_to_lds(pool_k + at, off + piece_k * 16, to_k);
+          request_to_lds(pool_v + at, off + piece_v * 16, to_v);
         } else {
-          const int visible = node - jn + 1;
-          nodes = visible >= 32 ? 0xffffffffu : visible > 0 ? (1u << visible) - 1 : 0u;
+          const int pos = pos0 + key0 + my_row;
+          const bool there = pos < total && page >= 0;
+          const int64_t at = 2 * (page * p.page_stride + (pos & in_page) * p.token_stride);
+          const char* from_k = there ? pool_k + at + piece_k * 16 : reinterpret_cast<const char*>(zero_piece);
+          const char* from_v = there ? pool_v + at + piece_v * 16 : reinterpret_cast<const char*>(zero_piece);
+          asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to_k), "v"(from_k) : "memory");
+          asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to_v), "v"(from_v) : "memory");
         }
-        const int committed = min(32, max(0, -j0));
-        seen = committed >= 32 ? 0xffffffffu : (1u << committed) - 1 | nodes << committed;
-        const int have = total - pos0;
-        if (have < 32) seen &= have > 0 ? (1u << have) - 1 : 0u;
       }
-      if (page0 < 0) seen &= 0xffff0000u;
-      if (page1 < 0) seen &= 0x0000ffffu;
+    };
+    auto page_of = [&](int granule, int half) {
+      return granule < g1 ? uniform_page(p, seq, (granule * KEYS + kw * 32 + half * 16) >> shift) : -1;
+    };
+
+    RowState<D> st;
+#pragma unroll
+    for (int b = 0; b < D / 32; b++) st.o[b] = f32x16{};
+    st.m = -INFINITY;
+    st.l = 0.f;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // from here on only the tiles' requests are in flight
+    __syncthreads();                                   // what was in the tiles has been read, and nothing is on its way there
+    unsigned none = 0;   // two bits per granule, the latest requested lowest: its first, last 16 keys are on no page
+#pragma unroll
+    for (int i = 0; i < STAGES - 1; i++) {
+      const int page0 = page_of(g0 + i, 0), page1 = page_of(g0 + i, 1);
+      none = none << 2 | (page1 < 0) << 1 | (page0 < 0);
+      request(g0 + i, i, page0, page1);
     }
-    const unsigned bits = seen >> (4 * h);   // bit 8 (i / 4) + i % 4 is register i's key
-    float top = -INFINITY;
+    int next0 = page_of(g0 + STAGES - 1, 0), next1 = page_of(g0 + STAGES - 1, 1);
+
+    int stage = 0;
+    bool odd_values = false;
+    for (int granule = g0; granule < g1; granule++) {
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"((STAGES - 2) * 2 * REQUESTS) : "memory");
+      __syncthreads();   // this granule is there, from every wave; the one before has been read by every wave
+      request(granule + STAGES - 1, stage == 0 ? STAGES - 1 : stage - 1, next0, next1);
+      none = none << 2 | (next1 < 0) << 1 | (next0 < 0);
+      next0 = page_of(granule + STAGES, 0), next1 = page_of(granule + STAGES, 1);
+      unsigned char* const tiles_v = tiles[stage][1][kw];
+      const unsigned lds_k = lds0 + (stage * 2 * KW + kw) * TILE, lds_v = lds_k + KW * TILE;
+      stage = stage + 1 == STAGES ? 0 : stage + 1;
+      const int pos0 = granule * KEYS + kw * 32;
+
+      // A weight of zero does not silence an infinity or a NaN.  Committed values are seen by every row; drafts' values that are no
+      // numbers are taken out here and given back, below, to the rows that see them.
+      if ((granule + 1) * KEYS > length) {
+        bool odd = false;
 #pragma unroll
-    for (int i = 0; i < 16; i++) {
-      s[i] *= a.scale;
-      if (!(bits >> (8 * (i >> 2) + (i & 3)) & 1)) s[i] = -INFINITY;
-      top = fmaxf(top, s[i]);
-    }
-    top = max_xor32(top);
-    const float m = fmaxf(st.m, top), safe = m == -INFINITY ? 0.f : m;
-    const float keep = __builtin_amdgcn_exp2f(st.m - safe);
-    st.m = m;
-    st.l *= keep;
+        for (int j = 0; j < REQUESTS; j++) odd |= clean<T, false>(tiles_v + (j * RW + rw) * 1024 + lane * 16);
+        if (__syncthreads_or(odd)) {
+          odd_values = true;
 #pragma unroll
-    for (int b = 0; b < D / 32; b++) st.o[b] *= keep;
-    s16x8 pf[2];
-#pragma unroll
-    for (int i = 0; i < 16; i++) {
-      const T w = (T)__builtin_amdgcn_exp2f(s[i] - safe);
-      pf[i >> 3][i & 7] = __builtin_bit_cast(short, w);
-      st.l += (float)w;   // what the product takes, so that rounding a dominant weight cancels
-    }
-    const unsigned char* vt = lds_v[kw];
-    bool odd_values = false;   // values that a weight of zero does not silence
-    if (drafts) {
-#pragma unroll
-      for (int i = 0; i < TILE / 1024; i++) {
-        const uint4 u = *reinterpret_cast<const uint4*>(vt + (i * 64 + lane) * 16);
-        const unsigned e = Mat<T>::EXPONENT, word[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-        for (int c = 0; c < 4; c++) odd_values |= (word[c] & e) == e || (word[c] >> 16 & e) == e;
+          for (int j = 0; j < REQUESTS; j++) (void)clean<T, true>(tiles_v + (j * RW + rw) * 1024 + lane * 16);
+          __syncthreads();
+        }
       }
-    }
-    if (__ballot(odd_values) == 0) {
-      const unsigned char* lane_v = vt + (4 * h + vkey) * (2 * D) + ((lane >> 4) & 1) * 32 + ((lane & 3) >> 1) * 16 + (lane & 1) * 8;
+
+      f32x16 s = {};
+#pragma unroll
+      for (int i = 0; i < D / 16; i++) {
+        const s16x8 kf = *((LdsPiece)(size_t)(lds_k + (read_k ^ ((2 * i & 14) << 4))) + (2 * i & 16));
+        s = Mat<T>::mfma(kf, q[i], s);
+      }
+      // what of the tile the row sees, a bit per key
+      unsigned seen = 0xffffffffu;
+      const bool drafts = pos0 + 32 > length;
+      const unsigned gone = none >> (2 * (STAGES - 1)) & 3;
+      if (drafts || gone != 0) {
+        const int j0 = pos0 - length;   // node at the tile's first key
+        if (drafts) {
+          unsigned nodes = 0;           // bit b: node max(j0, 0) + b
+          const int jn = max(j0, 0);
+          if (mask != nullptr) {
+            const int word = jn >> 5, off = jn & 31;
+            const unsigned lo = word < a.mask_words ? mask[word] : 0, hi = word + 1 < a.mask_words ? mask[word + 1] : 0;
+            nodes = (unsigned)(((unsigned long long)hi << 32 | lo) >> off);
+          } else {
+            const int visible = node - jn + 1;
+            nodes = visible >= 32 ? 0xffffffffu : visible > 0 ? (1u << visible) - 1 : 0u;
+          }
+          const int committed = min(32, max(0, -j0));
+          seen = committed >= 32 ? 0xffffffffu : (1u << committed) - 1 | nodes << committed;
+          const int have = total - pos0;
+          if (have < 32) seen &= have > 0 ? (1u << have) - 1 : 0u;
+        }
+        if (gone & 1) seen &= 0xffff0000u;
+        if (gone & 2) seen &= 0x0000ffffu;
+        const unsigned bits = seen >> (4 * h);   // bit 8 (i / 4) + i % 4 is register i's key
+#pragma unroll
+        for (int i = 0; i < 16; i++) s[i] = bits >> (8 * (i >> 2) + (i & 3)) & 1 ? s[i] : -INFINITY;
+      }
+      float top = s[0];
+#pragma unroll
+      for (int i = 1; i < 16; i++) top = fmaxf(top, s[i]);
+      top = max_xor32(top) * a.scale;
+      // The reference follows the maximum only where a weight would pass 2^(8 + HEADROOM): in the first tiles, hardly ever later.
+      // fp16 weights start at 2^HEADROOM, so that small ones keep their bits.
+      constexpr float HEADROOM = sizeof(T) == 2 && Mat<T>::EXPONENT == 0x7c00 ? 7.f : 0.f;
+      if (__ballot(top > st.m + (8.f + HEADROOM)) != 0) {
+        const float m = fmaxf(st.m, top - HEADROOM);
+        const float keep = st.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st.m - m);
+        st.m = m;
+        st.l *= keep;
+#pragma unroll
+        for (int b = 0; b < D / 32; b++) st.o[b] *= keep;
+      }
+      const float m = st.m == -INFINITY ? 0.f : st.m;
+      s16x8 pf[2];
+#pragma unroll
+      for (int i = 0; i < 16; i += 2) {
+        T2 w;
+        w[0] = (T)__builtin_amdgcn_exp2f(fmaf(s[i], a.scale, -m));
+        w[1] = (T)__builtin_amdgcn_exp2f(fmaf(s[i + 1], a.scale, -m));
+        st.l = dot_ones(w, st.l);   // of what the product takes, so that rounding a dominant weight cancels
+        pf[i >> 3][i & 7] = __builtin_bit_cast(short, (T)w[0]);
+        pf[i >> 3][(i & 7) + 1] = __builtin_bit_cast(short, (T)w[1]);
+      }
 #pragma unroll
       for (int b = 0; b < D / 32; b++) {
 #pragma unroll
         for (int step = 0; step < 2; step++) {
-          typedef __attribute__((address_space(3))) s16x4* LdsPtr;
-          const unsigned char* at = lane_v + ((b ^ swz_v) << 6) + step * 16 * 2 * D;
-          const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)(const s16x4*)at);
-          const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)(const s16x4*)(at + 8 * 2 * D));
+          const unsigned at = lds_v + (read_v ^ ((b & 3) << 6)) + (b >> 2) * 256 + step * 16 * 2 * D;
+          const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsQuad)(size_t)at);
+          const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsQuad)(size_t)(at + 8 * 2 * D));
           st.o[b] = Mat<T>::mfma(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7), pf[step], st.o[b]);
         }
       }
-    } else {
-      // Rare: a draft's values hold infinities or NaN.  Key by key, and only for the rows that see it.
-      float (*wt)[33] = weights[wave];
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the last requests, of nothing, write to the tiles as well
+    st.l = add_xor32(st.l);
+
+    // the KW groups' states into the first one's
+    if constexpr (KW > 1) {
+      static_assert(RW * (D / 2 + 2) * 256 <= STAGES * 2 * KW * TILE, "a state per row group fits the tiles");
+      float* const share = reinterpret_cast<float*>(tiles) + rw * (D / 2 + 2) * 64 + lane;   // [RW][D / 2 + 2][64]
+      for (int from = 1; from < KW; from++) {
+        __syncthreads();
+        if (kw == from) {
 #pragma unroll
-      for (int i = 0; i < 16; i++) {
-        const int key = 8 * (i >> 2) + 4 * h + (i & 3);
-        const short w = pf[i >> 3][i & 7];
-        wt[key][lane & 31] = seen >> key & 1 ? (float)__builtin_bit_cast(T, w) : -1.0f;
-      }
-      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-      __builtin_amdgcn_wave_barrier();
-      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-      for (int key = 0; key < 32; key++) {
-        const float w = wt[key][lane & 31];
-        if (w < 0.f) continue;
-        const int swz = D == 64 ? ((key >> 1) & 1) << 2 : (key & 3) << 2;
-        const unsigned char* row = vt + key * 2 * D + 8 * h;
+          for (int b = 0; b < D / 32; b++)
 #pragma unroll
-        for (int c = 0; c < D / 8; c++) {
-          const s16x4 v = *reinterpret_cast<const s16x4*>(row + ((c ^ swz) << 4));
+            for (int i = 0; i < 16; i++) share[(b * 16 + i) * 64] = st.o[b][i];
+          share[D / 2 * 64] = st.m;
+          share[(D / 2 + 1) * 64] = st.l;
+        }
+        __syncthreads();
+        if (kw == 0) {
+          const float om = share[D / 2 * 64], m = fmaxf(st.m, om), safe = m == -INFINITY ? 0.f : m;
+          const float c0 = __builtin_amdgcn_exp2f(st.m - safe), c1 = __builtin_amdgcn_exp2f(om - safe);
+          st.m = m;
+          st.l = st.l * c0 + share[(D / 2 + 1) * 64] * c1;
 #pragma unroll
-          for (int i = 0; i < 4; i++) st.o[c >> 2][(c & 3) * 4 + i] += w * (float)__builtin_bit_cast(T, (short)v[i]);
+          for (int b = 0; b < D / 32; b++)
+#pragma unroll
+            for (int i = 0; i < 16; i++) st.o[b][i] = st.o[b][i] * c0 + share[(b * 16 + i) * 64] * c1;
         }
       }
     }
-  }
-  st.l = add_xor32(st.l);
-
-  // the KW groups' states into the first one's
-  if (KW > 1) {
-    static_assert(KW == 1 || RW * (D / 2 + 2) * 256 <= 2 * KW * TILE, "a state per row group fits the tiles");
-    float* const share = reinterpret_cast<float*>(tiles);   // [RW][D / 32 * 16 + 2][64]; the tiles have been read
-    for (int from = 1; from < KW; from++) {
-      __syncthreads();
-      float* mine = share + rw * (D / 2 + 2) * 64 + lane;
-      if (kw == from) {
+    if (kw != 0 || !live) continue;
+    if (odd_values) {
+      // rare: sums that such values are part of are what adding them makes of any number
+#pragma unroll 1
+      for (int pos = max(length / KEYS, g0) * KEYS; pos < min(total, g1 * KEYS); pos++) {
+        const int j = pos - length, page = page_at(p, seq, pos >> shift);
+        const bool sees = j < 0 || (mask != nullptr ? (j >> 5) < a.mask_words && (mask[j >> 5] >> (j & 31) & 1) : j <= node);
+        if (!sees || page < 0) continue;
+        const T* row = reinterpret_cast<const T*>(pool_v) + page * p.page_stride + (pos & in_page) * p.token_stride + 4 * h;
 #pragma unroll
-        for (int b = 0; b < D / 32; b++)
+        for (int c = 0; c < D / 8; c++) {
+          const T4 v = *reinterpret_cast<const T4*>(row + c * 8);
 #pragma unroll
-          for (int i = 0; i < 16; i++) mine[(b * 16 + i) * 64] = st.o[b][i];
-        mine[D / 2 * 64] = st.m;
-        mine[(D / 2 + 1) * 64] = st.l;
-      }
-      __syncthreads();
-      if (kw == 0) {
-        const float om = mine[D / 2 * 64], m = fmaxf(st.m, om), safe = m == -INFINITY ? 0.f : m;
-        const float c0 = __builtin_amdgcn_exp2f(st.m - safe), c1 = __builtin_amdgcn_exp2f(om - safe);
-        st.m = m;
-        st.l = st.l * c0 + mine[(D / 2 + 1) * 64] * c1;
-#pragma unroll
-        for (int b = 0; b < D / 32; b++)
-#pragma unroll
-          for (int i = 0; i < 16; i++) st.o[b][i] = st.o[b][i] * c0 + mine[(b * 16 + i) * 64] * c1;
+          for (int i = 0; i < 4; i++) {
+            const float x = (float)v[i];
+            st.o[c >> 2][(c & 3) * 4 + i] += x - x == 0.f ? 0.f : x;
+          }
+        }
       }
     }
-  }
-  if (kw != 0 || !live) return;
-  const float inv = st.l == 0.f ? 0.f : 1.0f / st.l;
-  T* out = reinterpret_cast<T*>(a.out) + (rows.x + node) * a.out_row_stride + head * a.out_head_stride;
+    if (g0 == 0 && g1 == granules) {
+      const float inv = st.l == 0.f ? 0.f : 1.0f / st.l;
+      T* out = reinterpret_cast<T*>(a.out) + (rows.x + node) * a.out_row_stride + head * a.out_head_stride;
 #pragma unroll
-  for (int b = 0; b < D / 32; b++) {
+      for (int b = 0; b < D / 32; b++) {
 #pragma unroll
-    for (int i = 0; i < 16; i += 4) {
-      typedef T T4 __attribute__((ext_vector_type(4)));
-      T4 w;
+        for (int i = 0; i < 16; i += 4) {
+          T4 w;
 #pragma unroll
-      for (int c = 0; c < 4; c++) w[c] = (T)(st.o[b][i + c] * inv);
-      *reinterpret_cast<T4*>(out + b * 32 + 2 * i + 4 * h) = w;
+          for (int c = 0; c < 4; c++) w[c] = (T)(st.o[b][i + c] * inv);
+          *reinterpret_cast<T4*>(out + b * 32 + 2 * i + 4 * h) = w;
+        }
+      }
+    } else {
+      const size_t slot = ((size_t)blockIdx.x * 2 + (g0 == 0)) * ROWS + rw * 32 + (lane & 31);
+      float* out = a.part_o + slot * D;
+#pragma unroll
+      for (int b = 0; b < D / 32; b++) {
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+          f32x4 w;
+#pragma unroll
+          for (int c = 0; c < 4; c++) w[c] = st.o[b][i + c];
+          *reinterpret_cast<f32x4*>(out + b * 32 + 2 * i + 4 * h) = w;
+        }
+      }
+      if (h == 0) a.part_ml[slot] = make_float2(st.m, st.l);
     }
   }
 }
 
-template <class T, int D>
-void launch(hipStream_t s, TreeArgs& a) {
-  const int most = a.max_rows * a.group;
-  if (most <= 32) {
-    a.row_tiles = 1;
-    hipLaunchKernelGGL((tree_attention_kernel<T, D, 1, 2>), dim3(a.p.n_seqs * a.p.kv_heads), dim3(128), 0, s, a);
-  } else {
-    a.row_tiles = ceil_div(most, 128);
-    hipLaunchKernelGGL((tree_attention_kernel<T, D, 4, 1>), dim3(a.p.n_seqs * a.p.kv_heads * a.row_tiles), dim3(256), 0, s, a);
+// The rows of units that several blocks had a part in: sum_z 2^(m_z - m) o_z / sum_z 2^(m_z - m) l_z, in the order of the blocks.  One
+// block per row; its 8 waves share out the parts, D / 64 numbers per lane.
+constexpr int MERGE_WAVES = 8;
+template <class T, int D, int RW>
+__global__ __launch_bounds__(64 * MERGE_WAVES) void tree_merge_kernel(TreeArgs a) {
+  constexpr int ROWS = 32 * RW, KEYS = 32 * Shape<D, RW>::KW, PER = D / 64;
+  typedef float Vec __attribute__((ext_vector_type(PER)));
+  typedef T VecT __attribute__((ext_vector_type(PER)));
+  const pi0_pages& p = a.p;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int r = blockIdx.x, kv_head = blockIdx.y, seq = blockIdx.z;
+  const int2 rows = rows_of(a.row_start, seq, a.n_rows, a.max_rows);
+  if (r >= rows.y * a.group) return;
+  const int total = min(length_of(p, seq) + rows.y, p.max_pages * p.page_tokens);
+  const int granules = div_up(total, KEYS), row_tiles = div_up(rows.y * a.group, ROWS), row_tile = r / ROWS;
+  const int64_t run = a.prefix[p.n_seqs + 1], first = a.prefix[seq] + ((int64_t)kv_head * row_tiles + row_tile) * granules;
+  const int b0 = (int)(first / run), b1 = (int)((first + granules - 1) / run);
+  if (b0 == b1) return;
+  auto slot_of = [&](int block) { return ((size_t)block * 2 + (first >= block * run)) * ROWS + r % ROWS; };
+  float m = -INFINITY;
+  for (int b = b0 + (int)threadIdx.x; b <= b1; b += 64 * MERGE_WAVES) m = fmaxf(m, a.part_ml[slot_of(b)].x);
+  __shared__ float s_m[MERGE_WAVES], s_l[MERGE_WAVES];
+  __shared__ Vec s_o[MERGE_WAVES][64];
+  for (int i = 32; i > 0; i >>= 1) m = fmaxf(m, __shfl_xor(m, i));
+  if (lane == 0) s_m[wave] = m;
+  __syncthreads();
+  for (int w = 0; w < MERGE_WAVES; w++) m = fmaxf(m, s_m[w]);
+  const float safe = m == -INFINITY ? 0.f : m;
+  Vec o = {};
+  float l = 0.f;
+#pragma unroll 4
+  for (int b = b0 + wave; b <= b1; b += MERGE_WAVES) {
+    const size_t slot = slot_of(b);
+    const float2 ml = a.part_ml[slot];
+    const float c = __builtin_amdgcn_exp2f(ml.x - safe);
+    o += c * *reinterpret_cast<const Vec*>(a.part_o + slot * D + lane * PER);
+    l += c * ml.y;
   }
+  if (lane == 0) s_l[wave] = l;
+  s_o[wave][lane] = o;
+  __syncthreads();
+  if (wave != 0) return;
+  for (int w = 1; w < MERGE_WAVES; w++) o += s_o[w][lane], l += s_l[w];
+  const float inv = l == 0.f ? 0.f : 1.0f / l;
+  const int node = r / a.group, head = kv_head * a.group + r - node * a.group;
+  VecT w;
+#pragma unroll
+  for (int i = 0; i < PER; i++) w[i] = (T)(o[i] * inv);
+  *reinterpret_cast<VecT*>(reinterpret_cast<T*>(a.out) + (rows.x + node) * a.out_row_stride + head * a.out_head_stride + lane * PER) = w;
+}
+
+struct Space {
+  size_t prefix, part_ml, bytes;   // part_o lies in front
+};
+template <int D, int RW>
+Space space_of(const pi0_pages& p) {
+  Space s;
+  const size_t slots = (size_t)Shape<D, RW>::BLOCKS * 2 * 32 * RW;
+  s.part_ml = slots * D * sizeof(float);
+  s.prefix = s.part_ml + slots * sizeof(float2);
+  s.bytes = s.prefix + ((size_t)p.n_seqs + 2) * sizeof(int64_t);
+  return s;
+}
+
+// Row tiles of 32 where all rows of a sequence and key/value head fit one (single tokens, small drafts): its keys are read
+// once and the products have time to spare.  128 otherwise.
+bool few_rows(int max_rows, int group) { return max_rows * group <= 32; }
+
+template <int D>
+Space space_of(const pi0_pages& p, int heads, int max_rows) {
+  return few_rows(max_rows, heads / p.kv_heads) ? space_of<D, 1>(p) : space_of<D, 4>(p);
+}
+Space space_of(const pi0_pages& p, int heads, int max_rows) {
+  return p.head_dim == 64 ? space_of<64>(p, heads, max_rows) : p.head_dim == 128 ? space_of<128>(p, heads, max_rows) : space_of<256>(p, heads, max_rows);
+}
+
+template <class T, int D, int RW>
+void launch(hipStream_t s, TreeArgs& a, char* ws) {
+  const Space at = space_of<D, RW>(a.p);
+  a.part_o = reinterpret_cast<float*>(ws);
+  a.part_ml = reinterpret_cast<float2*>(ws + at.part_ml);
+  a.prefix = reinterpret_cast<int64_t*>(ws + at.prefix);
+  hipLaunchKernelGGL((tree_attention_kernel<T, D, RW>), dim3(Shape<D, RW>::BLOCKS), dim3(64 * RW * Shape<D, RW>::KW), 0, s, a);
+  hipLaunchKernelGGL((tree_merge_kernel<T, D, RW>), dim3(a.max_rows * a.group, a.p.kv_heads, a.p.n_seqs), dim3(64 * MERGE_WAVES), 0, s, a);
+}
+template <class T, int D>
+void launch(hipStream_t s, TreeArgs& a, char* ws) {
+  if (few_rows(a.max_rows, a.group)) launch<T, D, 1>(s, a, ws);
+  else launch<T, D, 4>(s, a, ws);
+}
+template <class T>
+void launch(hipStream_t s, TreeArgs& a, char* ws) {
+  if (a.p.head_dim == 64) launch<T, 64>(s, a, ws);
+  else if (a.p.head_dim == 128) launch<T, 128>(s, a, ws);
+  else launch<T, 256>(s, a, ws);
 }
 
 bool args_ok(const pi0_pages* p, int heads, int n_rows, int max_rows) {
@@ -302,7 +544,7 @@ bool args_ok(const pi0_pages* p, int heads, int n_rows, int max_rows) {
 extern "C" {
 
 size_t pi0_tree_attention_workspace_bytes(const pi0_pages* pages, int heads, int n_rows, int max_rows) {
-  return args_ok(pages, heads, n_rows, max_rows) ? 16 : 0;
+  return args_ok(pages, heads, n_rows, max_rows) ? space_of(*pages, heads, max_rows).bytes : 0;
 }
 
 int pi0_tree_attention(const pi0_pages* pages, int layer, const pi0_rows* q, const pi0_rows* out, const int32_t* d_row_start, int n_rows,
@@ -321,26 +563,23 @@ int pi0_tree_attention(const pi0_pages* pages, int layer, const pi0_rows* q, con
   a.q_head_stride = q->head_stride;
   a.out_row_stride = out->row_stride;
   a.out_head_stride = out->head_stride;
-  a.heads = q->heads;
   a.group = q->heads / pages->kv_heads;
   a.row_start = d_row_start;
   a.n_rows = n_rows;
   a.max_rows = max_rows;
   a.mask = d_mask;
   a.mask_words = mask_words;
-  a.scale = scale * 1.4426950408889634f;
+  a.scale = fabsf(scale) * 1.4426950408889634f;
+  a.negate = scale < 0.f ? (short)0x8000 : 0;
+  if (a.scale == 0.f) {   // all scores are zero, and so is what a masked one is compared with
+    a.zero = 1;
+    a.scale = 1.f;
+  }
+  a.near_rows = pages->token_stride < (int64_t)1 << 27;
   a.layer = layer * pages->layer_stride;
   hipStream_t s = reinterpret_cast<hipStream_t>(hip_stream);
-  const int d = pages->head_dim;
-  if (pages->dtype == PI0_BF16) {
-    if (d == 64) launch<bf16, 64>(s, a);
-    else if (d == 128) launch<bf16, 128>(s, a);
-    else launch<bf16, 256>(s, a);
-  } else {
-    if (d == 64) launch<f16, 64>(s, a);
-    else if (d == 128) launch<f16, 128>(s, a);
-    else launch<f16, 256>(s, a);
-  }
+  if (pages->dtype == PI0_BF16) launch<bf16>(s, a, reinterpret_cast<char*>(d_workspace));
+  else launch<f16>(s, a, reinterpret_cast<char*>(d_workspace));
   return hipGetLastError() == hipSuccess ? PI0_OK : PI0_EHIP;
 }
 

@@ -190,6 +190,17 @@ def test_what_is_not_seen_may_be_anything(dtype, d):
         assert np.abs(mine[fine] - want[fine]).max() <= 2.0 ** -7 * 6
 
 
+def test_committed_values_that_are_no_numbers_reach_every_row():
+    for at in (3, 36):                        # in a tile of its own, and in one that drafts begin in
+        c = Case(75, [37], [6], 8, 2, 128, 16, "bf16")
+        c.pages.v[0, int(c.table[0, at // 16]), at % 16, 1, 5] = float("-inf")
+        c.run()
+        got = f64(c.out)[c.starts[0]:c.starts[1]]
+        assert np.isneginf(got[:, 4:, 5]).all()
+        got[:, 4:, 5] = 0
+        assert np.isfinite(got).all()
+
+
 def test_positions_without_a_page_are_not_seen():
     c = Case(80, [100, 64], [4, 4], 8, 1, 256, 16, "bf16")
     c.pages.table[0, 2] = -1
