@@ -51,7 +51,7 @@ struct TreeArgs {
   int mask_words;
   float scale;           // times log2(e), >= 0
   short negate;          // 0x8000 where the queries' signs are turned instead of the scale's
-  short zero;            // queries are all zero (scale 0)
+  short q_bits;          // 0 where the queries are taken as zero (scale 0)
   int near_rows;         // eight rows of a page lie within 32 bits of offsets
   int64_t layer;         // elements in front of the layer
   // workspace
@@ -99,6 +99,24 @@ struct RowState {
 
 __device__ __forceinline__ float dot_ones(bf16x2 w, float c) { return __builtin_amdgcn_fdot2_f32_bf16(w, bf16x2{(bf16)1.0f, (bf16)1.0f}, c, false); }
 __device__ __forceinline__ float dot_ones(f16x2 w, float c) { return __builtin_amdgcn_fdot2(w, f16x2{(f16)1.0f, (f16)1.0f}, c, false); }
+
+// o *= c, where it is: in the accumulation registers.  Written as a product, the sums are copied to vector registers in every round, whether
+// or not the branch is taken (128 instructions at D = 256).  The products that wrote them have long ended - the scores
+// that decided the branch are a later product's - and the waits in front and behind cover the longest there is.
+template <int N>
+__device__ __forceinline__ void scale_sums(f32x16 (&o)[N], float c) {
+  asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
+#pragma unroll
+  for (int b = 0; b < N; b++) {
+#pragma unroll
+    for (int i = 0; i < 16; i++) {
+      float x = o[b][i], t;
+      asm volatile("v_accvgpr_read_b32 %1, %0\n\tv_mul_f32 %1, %1, %2\n\tv_accvgpr_write_b32 %0, %1" : "+a"(x), "=&v"(t) : "v"(c));
+      o[b][i] = x;
+    }
+  }
+  asm volatile("s_nop 15" ::: "memory");
+}
 
 // whether 16 bytes of LDS hold an infinity or a NaN; CLEAN: puts zeros in their place
 template <class T, bool CLEAN>
@@ -199,13 +217,12 @@ __global__ __launch_bounds__((64 * RW * Shape<D, RW>::KW)) void tree_attention_k
     const int r = row_tile * ROWS + rw * 32 + (lane & 31);
     const bool live = r < rows.y * a.group;
     const int node = live ? r / a.group : 0, head = kv_head * a.group + (live ? r - node * a.group : 0);
-    s16x8 q[D / 16];
+    s16x8 q[D / 16];   // (a lane without a row takes the tile's first token's, and gives nothing back)
+    const T* const q_row = reinterpret_cast<const T*>(a.q) + (rows.x + node) * a.q_row_stride + head * a.q_head_stride + h * 8;
 #pragma unroll
-    for (int i = 0; i < D / 16; i++) {
-      q[i] = s16x8{};
-      if (live && !a.zero)
-        q[i] = *reinterpret_cast<const s16x8*>(reinterpret_cast<const T*>(a.q) + (rows.x + node) * a.q_row_stride + head * a.q_head_stride + i * 16 + h * 8) ^ a.negate;
-    }
+    for (int i = 0; i < D / 16; i++) q[i] = *reinterpret_cast<const s16x8*>(q_row + i * 16);
+#pragma unroll
+    for (int i = 0; i < D / 16; i++) q[i] = (q[i] ^ a.negate) & a.q_bits;
     const unsigned* mask = a.mask != nullptr ? a.mask + (size_t)(rows.x + node) * a.mask_words : nullptr;
     const char* const pool_k = reinterpret_cast<const char*>(p.d_k) + 2 * (a.layer + kv_head * p.head_stride);
     const char* const pool_v = reinterpret_cast<const char*>(p.d_v) + 2 * (a.layer + kv_head * p.head_stride);
@@ -215,26 +232,30 @@ __global__ __launch_bounds__((64 * RW * Shape<D, RW>::KW)) void tree_attention_k
     auto request = [&](int granule, int stage, int page0, int page1) {
       const int pos0 = granule * KEYS + kw * 32;
       const unsigned to = lds0 + ((stage * 2) * KW + kw) * TILE;
-      const bool whole = pos0 + 32 <= total && page0 >= 0 && page1 >= 0 && a.near_rows;
+      if (pos0 + 32 <= total && page0 >= 0 && page1 >= 0 && a.near_rows) {
+        const int64_t at0 = 2 * (page0 * p.page_stride + (pos0 & in_page) * p.token_stride);
+        const int64_t at1 = 2 * (page1 * p.page_stride + ((pos0 + 16) & in_page) * p.token_stride);
+        const unsigned off = my_row * (unsigned)(2 * p.token_stride);
 #pragma unroll
-      for (int j = 0; j < REQUESTS; j++) {
-        const int part = j * RW + rw, key0 = part * KEYS_PER_REQUEST;   // the KiB and its first key
-        const int page = key0 < 16 ? page0 : page1;
-        const unsigned to_k = to + part * 1024, to_v = to_k + KW * TILE;
-        const int piece_k = piece_k0 ^ (D == 64 ? (key0 >> 1) & 7 : key0 & 15), piece_v = piece_v0 ^ (D == 64 ? ((key0 >> 1) & 1) << 2 : (key0 & 3) << 2);
-        if (whole) {
-          const int64_t at = 2 * (page * p.page_stride + ((pos0 + key0) & in_page) * p.token_stride);
-          const unsigned off = my_row * (unsigned)(2 * p.token_stride);
-          request_to_lds(pool_k + at, off + piece_k * 16, to_k);
-          request_to_lds(pool_v + at, off + piece_v * 16, to_v);
-        } else {
-          const int pos = pos0 + key0 + my_row;
+        for (int j = 0; j < REQUESTS; j++) {
+          const int part = j * RW + rw, key0 = part * KEYS_PER_REQUEST;   // the KiB and its first key
+          const int64_t at = (key0 < 16 ? at0 : at1) + (key0 & 15) * (2 * p.token_stride);
+          const int turn_k = D == 64 ? (key0 >> 1) & 7 : key0 & 15, turn_v = D == 64 ? ((key0 >> 1) & 1) << 2 : (key0 & 3) << 2;
+          request_to_lds(pool_k + at, off + (piece_k0 ^ turn_k) * 16, to + part * 1024);
+          request_to_lds(pool_v + at, off + (piece_v0 ^ turn_v) * 16, to + KW * TILE + part * 1024);
+        }
+      } else {
+#pragma unroll 1
+        for (int j = 0; j < REQUESTS; j++) {
+          const int part = j * RW + rw, key0 = part * KEYS_PER_REQUEST;
+          const int page = key0 < 16 ? page0 : page1, pos = pos0 + key0 + my_row;
           const bool there = pos < total && page >= 0;
           const int64_t at = 2 * (page * p.page_stride + (pos & in_page) * p.token_stride);
-          const char* from_k = there ? pool_k + at + piece_k * 16 : reinterpret_cast<const char*>(zero_piece);
-          const char* from_v = there ? pool_v + at + piece_v * 16 : reinterpret_cast<const char*>(zero_piece);
-          asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to_k), "v"(from_k) : "memory");
-          asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to_v), "v"(from_v) : "memory");
+          const int turn_k = D == 64 ? (key0 >> 1) & 7 : key0 & 15, turn_v = D == 64 ? ((key0 >> 1) & 1) << 2 : (key0 & 3) << 2;
+          const char* from_k = there ? pool_k + at + (piece_k0 ^ turn_k) * 16 : reinterpret_cast<const char*>(zero_piece);
+          const char* from_v = there ? pool_v + at + (piece_v0 ^ turn_v) * 16 : reinterpret_cast<const char*>(zero_piece);
+          asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to + part * 1024), "v"(from_k) : "memory");
+          asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to + KW * TILE + part * 1024), "v"(from_v) : "memory");
         }
       }
     };
@@ -331,8 +352,7 @@ __global__ __launch_bounds__((64 * RW * Shape<D, RW>::KW)) void tree_attention_k
         const float keep = st.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st.m - m);
         st.m = m;
         st.l *= keep;
-#pragma unroll
-        for (int b = 0; b < D / 32; b++) st.o[b] *= keep;
+        scale_sums<D / 32>(st.o, keep);
       }
       const float m = st.m == -INFINITY ? 0.f : st.m;
       s16x8 pf[2];
@@ -571,8 +591,9 @@ int pi0_tree_attention(const pi0_pages* pages, int layer, const pi0_rows* q, con
   a.mask_words = mask_words;
   a.scale = fabsf(scale) * 1.4426950408889634f;
   a.negate = scale < 0.f ? (short)0x8000 : 0;
-  if (a.scale == 0.f) {   // all scores are zero, and so is what a masked one is compared with
-    a.zero = 1;
+  a.q_bits = -1;
+  if (a.scale == 0.f) {   // all scores are zero, and a masked one stays minus infinity
+    a.q_bits = 0;
     a.scale = 1.f;
   }
   a.near_rows = pages->token_stride < (int64_t)1 << 27;
