@@ -5,6 +5,8 @@
 
 typedef _Float16 f16;
 
+constexpr int MAX_SEQS = 1024;   // sequences of a cache
+
 // what the host can check of a cache without looking at device memory
 bool pages_ok(const pi0_pages* p);
 // rows of `heads` heads (0: any number) of `head_dim` elements in type `dtype`

@@ -39,6 +39,42 @@ struct Mat<f16> {
   }
 };
 
+
+// How the work is cut.  A unit is a tile of 32 RW rows of one sequence and key/value head against all of its keys, in granules of 32
+// keys.  Lengths differ, and the host does not know them, so every block works out from the lengths which granules are its
+// own: the units lie behind each other in the order (sequence, head, row tile) on a line that is cut into runs of equal length,
+// one per block.
+//   - Few units (at most half as many as blocks): each takes up a whole number of runs, so that a block has part of one unit
+//     only; the shortest run for which there are blocks enough, of nine between the least and twice that.
+//   - Many: the line is dense, except that a unit is START granules longer than it is - what a block spends before a unit's
+//     first granule and behind its last -, and a run may end one unit, hold others and begin the next.
+// A block writes a unit that it has all of; of any other it leaves a partial result, in slot 0 if its run begins inside of the
+// unit, in slot 1 if the unit begins inside the run, and the second launch joins them.
+constexpr int GRANULE = 32, START = 6;
+
+// A stage of K and V tiles is 128 D bytes; STAGES of them per block.  With one row tile per wave and 256 d the registers hold one
+// wave per SIMD.  Few rows: what counts is bytes in flight and, beside them, other blocks that read while one begins or
+// ends a unit, so blocks are small and several share a compute unit.  BLOCKS: as many as the chip's 256 hold at once.
+template <int D, int RW>
+struct Shape;
+template <> struct Shape<256, 1> { static constexpr int STAGES = 2, BLOCKS = 512; };
+template <> struct Shape<256, 2> { static constexpr int STAGES = 2, BLOCKS = 512; };
+template <> struct Shape<256, 4> { static constexpr int STAGES = 4, BLOCKS = 256; };
+template <> struct Shape<128, 1> { static constexpr int STAGES = 2, BLOCKS = 1024; };
+template <> struct Shape<128, 2> { static constexpr int STAGES = 4, BLOCKS = 512; };
+template <> struct Shape<128, 4> { static constexpr int STAGES = 4, BLOCKS = 512; };
+template <> struct Shape<64, 1> { static constexpr int STAGES = 4, BLOCKS = 1024; };
+template <> struct Shape<64, 2> { static constexpr int STAGES = 4, BLOCKS = 1024; };
+template <> struct Shape<64, 4> { static constexpr int STAGES = 4, BLOCKS = 512; };
+
+// Where a unit lies on the line.  length: of the unit's share of the line, front: how far behind its beginning the first granule is
+struct Cut {
+  int64_t run;
+  int whole;   // units take up whole runs
+  __device__ __forceinline__ int64_t length(int granules) const { return whole ? (granules + run - 1) / run * run : granules > 0 ? granules + START : 0; }
+  __device__ __forceinline__ int front() const { return whole ? 0 : START; }
+};
+
 struct TreeArgs {
   pi0_pages p;
   const void* q;
@@ -55,32 +91,17 @@ struct TreeArgs {
   int near_rows;         // eight rows of a page lie within 32 bits of offsets
   int64_t layer;         // elements in front of the layer
   // workspace
-  int64_t* prefix;       // [n_seqs + 1] granules in front of a sequence, [n_seqs + 1] granules per block
+  int64_t* upto;         // [n_seqs] where a sequence's share of the line ends
+  Cut* cut;
   float* part_o;         // [blocks][2][rows of a tile][head_dim]
-  float2* part_ml;       // [blocks][2][rows of a tile]
+  float2* part_ml;       // [blocks][2][rows of a tile]: reference of the exponents, sum of the weights
 };
-
-// How the work is cut.  A unit is 32 RW rows of one sequence and key/value head against all of its keys, in granules of 32 KW keys.
-// The granules of all units, in the order (sequence, head, row tile, granule), are dealt out to the blocks in equal runs: lengths differ,
-// and the host does not know them.  A block writes a unit that lies in its run as a whole; of the unit that its run begins inside of
-// it leaves a partial result in slot 0, of the one that goes on behind its run in slot 1, for the second launch.
-template <int D, int RW>
-struct Shape;
-// K and V tiles of a stage are KW x 64 D x 2 bytes; STAGES of them fill 128 KB where a row tile is 32 rows (bytes in
-// flight are what the speed is made of there)
-template <> struct Shape<256, 1> { static constexpr int KW = 2, STAGES = 2, BLOCKS = 256; };
-template <> struct Shape<128, 1> { static constexpr int KW = 4, STAGES = 2, BLOCKS = 256; };
-template <> struct Shape<64, 1> { static constexpr int KW = 4, STAGES = 4, BLOCKS = 256; };
-template <> struct Shape<256, 4> { static constexpr int KW = 1, STAGES = 4, BLOCKS = 256; };
-template <> struct Shape<128, 4> { static constexpr int KW = 1, STAGES = 4, BLOCKS = 512; };
-template <> struct Shape<64, 4> { static constexpr int KW = 1, STAGES = 4, BLOCKS = 512; };
 
 // page_at for a sequence and entry that are the same for the whole wave: through the scalar cache, so that it does not
 // wait in line behind the tiles that are on their way
 __device__ __forceinline__ int uniform_page(const pi0_pages& p, int seq, int idx) {
-  if (idx >= p.max_pages) return -1;
-  const int page = ((const __attribute__((address_space(4))) int*)p.d_table)[(size_t)seq * p.max_pages + idx];
-  return page >= 0 && page < p.n_pages ? page : -1;
+  const int page = ((const __attribute__((address_space(4))) int*)p.d_table)[(size_t)seq * p.max_pages + min(idx, p.max_pages - 1)];
+  return idx < p.max_pages && page >= 0 && page < p.n_pages ? page : -1;
 }
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
@@ -135,54 +156,100 @@ __device__ __forceinline__ bool clean(unsigned char* at) {
   return odd;
 }
 
-// T: type; RW waves side by side have 32 rows each, KW of those groups a tile of 32 keys each
+// RW waves of a block have 32 rows each and read the same tiles
 template <class T, int D, int RW>
-__global__ __launch_bounds__((64 * RW * Shape<D, RW>::KW)) void tree_attention_kernel(TreeArgs a) {
-  constexpr int KW = Shape<D, RW>::KW, STAGES = Shape<D, RW>::STAGES, WAVES = RW * KW, THREADS = 64 * WAVES;
-  constexpr int PIECES = D / 8, TILE = 32 * D * 2, REQUESTS = TILE / 1024 / RW, KEYS_PER_REQUEST = 512 / D;
-  constexpr int ROWS = 32 * RW, KEYS = 32 * KW;
+__global__ __launch_bounds__(64 * RW) void tree_attention_kernel(TreeArgs a) {
+  constexpr int STAGES = Shape<D, RW>::STAGES, BLOCKS = Shape<D, RW>::BLOCKS, THREADS = 64 * RW;
+  constexpr int PIECES = D / 8, TILE = 32 * D * 2, REQUESTS = TILE / 1024 / RW, KEYS_PER_REQUEST = 512 / D, ROWS = 32 * RW;
   static_assert(REQUESTS >= 1 && STAGES >= 2 && (STAGES - 2) * 2 * REQUESTS < 64, "the wait counter holds what is in flight");
   typedef T T2 __attribute__((ext_vector_type(2)));
   typedef T T4 __attribute__((ext_vector_type(4)));
   const pi0_pages& p = a.p;
-  __shared__ __align__(1024) unsigned char tiles[STAGES][2][KW][TILE];
-  __shared__ int64_t prefix[1025];
-  __shared__ int64_t sums[WAVES];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int rw = wave % RW, kw = wave / RW, h = lane >> 5;
+  __shared__ __align__(1024) unsigned char tiles[STAGES][2][TILE];
+  __shared__ int64_t upto[MAX_SEQS];   // where each sequence's share of the line ends
+  int64_t (*const sums)[10] = reinterpret_cast<int64_t (*)[10]>(tiles);   // before there are any tiles
+  const int lane = threadIdx.x & 63, rw = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
 
-  // granules in front of each sequence
+  // The line: units, granules and, for nine lengths of a run, how many blocks they ask for
+  Cut cut;
   {
-    const int per_thread = div_up(p.n_seqs, THREADS), s0 = threadIdx.x * per_thread;
-    int64_t mine = 0;
-    for (int s = s0; s < min(p.n_seqs, s0 + per_thread); s++) {
+    const int per_thread = div_up(p.n_seqs, THREADS), s0 = threadIdx.x * per_thread, s1 = min(p.n_seqs, s0 + per_thread);
+    auto reduce = [&](int64_t (&v)[9], int n) {
+      for (int k = 0; k < n; k++) {
+        for (int i = 32; i > 0; i >>= 1) v[k] += __shfl_xor(v[k], i);
+      }
+      if constexpr (RW > 1) {
+        __syncthreads();
+        for (int k = 0; k < n; k++) {
+          if (lane == 0) sums[rw][k] = v[k];
+        }
+        __syncthreads();
+        for (int k = 0; k < n; k++) {
+          v[k] = 0;
+          for (int w = 0; w < RW; w++) v[k] += sums[w][k];
+        }
+      }
+    };
+    auto units_of = [&](int s, int* granules) {
       const int n = rows_of(a.row_start, s, a.n_rows, a.max_rows).y;
-      const int total = min(length_of(p, s) + n, p.max_pages * p.page_tokens);
-      prefix[s + 1] = (int64_t)p.kv_heads * div_up(n * a.group, ROWS) * div_up(total, KEYS);
-      mine += prefix[s + 1];
+      *granules = div_up(min(length_of(p, s) + n, p.max_pages * p.page_tokens), GRANULE);
+      return (int64_t)p.kv_heads * div_up(n * a.group, ROWS);
+    };
+    int64_t v[9] = {};
+    for (int s = s0; s < s1; s++) {
+      int granules;
+      const int64_t units = units_of(s, &granules);
+      v[0] += units;
+      v[1] += units * granules;
+      upto[s] = units << 32 | granules;   // (its place in between; units are at most kv_heads * 1024 * 1024 / 32)
     }
-    int64_t upto = mine;
+    reduce(v, 2);
+    const int64_t least = max((int64_t)1, (v[1] + BLOCKS - 1) / BLOCKS);
+    cut.whole = v[0] <= BLOCKS / 2;
+    cut.run = max((int64_t)1, (v[1] + v[0] * START + BLOCKS - 1) / BLOCKS);
+    if (cut.whole) {
+      for (int k = 0; k < 9; k++) v[k] = 0;
+      for (int s = s0; s < s1; s++) {
+        const int64_t units = upto[s] >> 32;
+        const int granules = (int)upto[s];
+        for (int k = 0; k < 9; k++) {
+          const unsigned run = (unsigned)(least + (least * k + 7) / 8);
+          v[k] += units * ((granules + run - 1) / run);
+        }
+      }
+      reduce(v, 9);
+      cut.run = 2 * least;
+      for (int k = 7; k >= 0; k--) {
+        if (v[k] <= BLOCKS) cut.run = least + (least * k + 7) / 8;
+      }
+    }
+    int64_t mine = 0;
+    for (int s = s0; s < s1; s++) {
+      upto[s] = (upto[s] >> 32) * cut.length((int)upto[s]);
+      mine += upto[s];
+    }
+    int64_t sum = mine;
     for (int i = 1; i < 64; i <<= 1) {
-      const int64_t u = __shfl_up(upto, i);
-      if (lane >= i) upto += u;
+      const int64_t u = __shfl_up(sum, i);
+      if (lane >= i) sum += u;
     }
-    if (lane == 63) sums[wave] = upto;
-    __syncthreads();
-    for (int w = 0; w < wave; w++) upto += sums[w];
-    int64_t before = upto - mine;
-    if (threadIdx.x == 0) prefix[0] = 0;
-    for (int s = s0; s < min(p.n_seqs, s0 + per_thread); s++) {
-      before += prefix[s + 1];
-      prefix[s + 1] = before;
+    if constexpr (RW > 1) {
+      if (lane == 63) sums[rw][9] = sum;
+      __syncthreads();
+      for (int w = 0; w < rw; w++) sum += sums[w][9];
+    }
+    int64_t before = sum - mine;
+    for (int s = s0; s < s1; s++) {
+      before += upto[s];
+      upto[s] = before;
     }
     __syncthreads();
   }
-  const int64_t all = prefix[p.n_seqs], run = max((int64_t)1, (all + gridDim.x - 1) / gridDim.x);
   if (blockIdx.x == 0) {
-    for (int s = threadIdx.x; s <= p.n_seqs; s += THREADS) a.prefix[s] = prefix[s];
-    if (threadIdx.x == 0) a.prefix[p.n_seqs + 1] = run;
+    for (int s = threadIdx.x; s < p.n_seqs; s += THREADS) a.upto[s] = upto[s];
+    if (threadIdx.x == 0) *a.cut = cut;
   }
-  const int64_t begin = blockIdx.x * run, end = min(all, begin + run);
+  const int64_t begin = blockIdx.x * cut.run, end = min(upto[p.n_seqs - 1], begin + cut.run);
 
   // This lane's pieces.  First product: key lane % 32, pieces h, h + 2, ..; second: of 4 keys and 16 d that 16 lanes read transposed,
   // key (lane % 16) / 4 and quad lane % 4.  Requests: row lane / PIECES of a KiB, its piece lane % PIECES - where the row's
@@ -193,25 +260,30 @@ __global__ __launch_bounds__((64 * RW * Shape<D, RW>::KW)) void tree_attention_k
   const int my_row = lane / PIECES, my_piece = lane % PIECES;
   const int piece_k0 = my_piece ^ (D == 64 ? (my_row >> 1) & 7 : my_row), piece_v0 = my_piece ^ (D == 64 ? ((my_row >> 1) & 1) << 2 : (my_row & 3) << 2);
   const int shift = 31 - __clz(p.page_tokens), in_page = p.page_tokens - 1;
-  const unsigned lds0 = lds_address(&tiles[0][0][0][0]);
+  const unsigned lds0 = lds_address(&tiles[0][0][0]);
 
   for (int64_t cur = begin; cur < end;) {
     // the unit that this run is in
     int seq = 0;
-    for (int top = p.n_seqs; top - seq > 1;) {
+    for (int top = p.n_seqs - 1; seq < top;) {
       const int mid = (seq + top) >> 1;
-      if (prefix[mid] <= cur) seq = mid;
+      if (upto[mid] <= cur) seq = mid + 1;
       else top = mid;
     }
     seq = uniform(seq);
+    const int64_t before = seq > 0 ? upto[seq - 1] : 0;
     const int2 rows = rows_of(a.row_start, seq, a.n_rows, a.max_rows);
     const int length = uniform(length_of(p, seq)), total = uniform(min(length + rows.y, p.max_pages * p.page_tokens));
-    const int granules = div_up(total, KEYS), row_tiles = uniform(div_up(rows.y * a.group, ROWS));
-    const int64_t inside = cur - prefix[seq];
-    const int unit = uniform((int)(inside / granules)), g0 = uniform((int)(inside - (int64_t)unit * granules));
-    const int g1 = uniform((int)min((int64_t)granules, g0 + (end - cur)));
+    const int granules = div_up(total, GRANULE), row_tiles = uniform(div_up(rows.y * a.group, ROWS));
+    const int64_t inside = cur - before, room = cut.length(granules);
+    int unit = (int)((double)inside / (double)room);   // right to one: the quotient is below 2^31
+    unit += inside - unit * room >= room;
+    unit = uniform(unit - (inside < unit * room));
+    const int64_t first = before + unit * room + cut.front();
+    const int g0 = uniform((int)max((int64_t)0, cur - first)), g1 = uniform((int)min((int64_t)granules, end - first));
     const int kv_head = unit / row_tiles, row_tile = unit - kv_head * row_tiles;
-    cur += g1 - g0;
+    cur = before + (unit + 1) * room;
+    if (g0 >= g1) continue;   // the run ends in front of the unit's first granule, or begins behind its last
 
     // this lane's row: token and head
     const int r = row_tile * ROWS + rw * 32 + (lane & 31);
@@ -230,8 +302,8 @@ __global__ __launch_bounds__((64 * RW * Shape<D, RW>::KW)) void tree_attention_k
     // Requests this wave's part of a granule, of whose keys the first and last 16 lie in pages page0 and page1 (-1: none; a granule
     // behind the last is asked for as well, as zeros, so that as many requests are in flight at the end as anywhere).
     auto request = [&](int granule, int stage, int page0, int page1) {
-      const int pos0 = granule * KEYS + kw * 32;
-      const unsigned to = lds0 + ((stage * 2) * KW + kw) * TILE;
+      const int pos0 = granule * GRANULE;
+      const unsigned to = lds0 + stage * 2 * TILE;
       if (pos0 + 32 <= total && page0 >= 0 && page1 >= 0 && a.near_rows) {
         const int64_t at0 = 2 * (page0 * p.page_stride + (pos0 & in_page) * p.token_stride);
         const int64_t at1 = 2 * (page1 * p.page_stride + ((pos0 + 16) & in_page) * p.token_stride);
@@ -242,7 +314,7 @@ __global__ __launch_bounds__((64 * RW * Shape<D, RW>::KW)) void tree_attention_k
           const int64_t at = (key0 < 16 ? at0 : at1) + (key0 & 15) * (2 * p.token_stride);
           const int turn_k = D == 64 ? (key0 >> 1) & 7 : key0 & 15, turn_v = D == 64 ? ((key0 >> 1) & 1) << 2 : (key0 & 3) << 2;
           request_to_lds(pool_k + at, off + (piece_k0 ^ turn_k) * 16, to + part * 1024);
-          request_to_lds(pool_v + at, off + (piece_v0 ^ turn_v) * 16, to + KW * TILE + part * 1024);
+          request_to_lds(pool_v + at, off + (piece_v0 ^ turn_v) * 16, to + TILE + part * 1024);
         }
       } else {
 #pragma unroll 1
@@ -255,12 +327,13 @@ __global__ __launch_bounds__((64 * RW * Shape<D, RW>::KW)) void tree_attention_k
           const char* from_k = there ? pool_k + at + (piece_k0 ^ turn_k) * 16 : reinterpret_cast<const char*>(zero_piece);
           const char* from_v = there ? pool_v + at + (piece_v0 ^ turn_v) * 16 : reinterpret_cast<const char*>(zero_piece);
           asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to + part * 1024), "v"(from_k) : "memory");
-          asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to + KW * TILE + part * 1024), "v"(from_v) : "memory");
+          asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to + TILE + part * 1024), "v"(from_v) : "memory");
         }
       }
     };
     auto page_of = [&](int granule, int half) {
-      return granule < g1 ? uniform_page(p, seq, (granule * KEYS + kw * 32 + half * 16) >> shift) : -1;
+      const int page = uniform_page(p, seq, (granule * GRANULE + half * 16) >> shift);
+      return granule < g1 ? page : -1;
     };
 
     RowState<D> st;
@@ -271,13 +344,15 @@ __global__ __launch_bounds__((64 * RW * Shape<D, RW>::KW)) void tree_attention_k
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // from here on only the tiles' requests are in flight
     __syncthreads();                                   // what was in the tiles has been read, and nothing is on its way there
     unsigned none = 0;   // two bits per granule, the latest requested lowest: its first, last 16 keys are on no page
+    int pages[STAGES][2];
+#pragma unroll
+    for (int i = 0; i < STAGES; i++) pages[i][0] = page_of(g0 + i, 0), pages[i][1] = page_of(g0 + i, 1);
 #pragma unroll
     for (int i = 0; i < STAGES - 1; i++) {
-      const int page0 = page_of(g0 + i, 0), page1 = page_of(g0 + i, 1);
-      none = none << 2 | (page1 < 0) << 1 | (page0 < 0);
-      request(g0 + i, i, page0, page1);
+      none = none << 2 | (pages[i][1] < 0) << 1 | (pages[i][0] < 0);
+      request(g0 + i, i, pages[i][0], pages[i][1]);
     }
-    int next0 = page_of(g0 + STAGES - 1, 0), next1 = page_of(g0 + STAGES - 1, 1);
+    int next0 = pages[STAGES - 1][0], next1 = pages[STAGES - 1][1];
 
     int stage = 0;
     bool odd_values = false;
@@ -287,14 +362,14 @@ __global__ __launch_bounds__((64 * RW * Shape<D, RW>::KW)) void tree_attention_k
       request(granule + STAGES - 1, stage == 0 ? STAGES - 1 : stage - 1, next0, next1);
       none = none << 2 | (next1 < 0) << 1 | (next0 < 0);
       next0 = page_of(granule + STAGES, 0), next1 = page_of(granule + STAGES, 1);
-      unsigned char* const tiles_v = tiles[stage][1][kw];
-      const unsigned lds_k = lds0 + (stage * 2 * KW + kw) * TILE, lds_v = lds_k + KW * TILE;
+      unsigned char* const tiles_v = tiles[stage][1];
+      const unsigned lds_k = lds0 + stage * 2 * TILE, lds_v = lds_k + TILE;
       stage = stage + 1 == STAGES ? 0 : stage + 1;
-      const int pos0 = granule * KEYS + kw * 32;
+      const int pos0 = granule * GRANULE;
 
       // A weight of zero does not silence an infinity or a NaN.  Committed values are seen by every row; drafts' values that are no
       // numbers are taken out here and given back, below, to the rows that see them.
-      if ((granule + 1) * KEYS > length) {
+      if (pos0 + GRANULE > length) {
         bool odd = false;
 #pragma unroll
         for (int j = 0; j < REQUESTS; j++) odd |= clean<T, false>(tiles_v + (j * RW + rw) * 1024 + lane * 16);
@@ -379,38 +454,11 @@ __global__ __launch_bounds__((64 * RW * Shape<D, RW>::KW)) void tree_attention_k
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the last requests, of nothing, write to the tiles as well
     st.l = add_xor32(st.l);
 
-    // the KW groups' states into the first one's
-    if constexpr (KW > 1) {
-      static_assert(RW * (D / 2 + 2) * 256 <= STAGES * 2 * KW * TILE, "a state per row group fits the tiles");
-      float* const share = reinterpret_cast<float*>(tiles) + rw * (D / 2 + 2) * 64 + lane;   // [RW][D / 2 + 2][64]
-      for (int from = 1; from < KW; from++) {
-        __syncthreads();
-        if (kw == from) {
-#pragma unroll
-          for (int b = 0; b < D / 32; b++)
-#pragma unroll
-            for (int i = 0; i < 16; i++) share[(b * 16 + i) * 64] = st.o[b][i];
-          share[D / 2 * 64] = st.m;
-          share[(D / 2 + 1) * 64] = st.l;
-        }
-        __syncthreads();
-        if (kw == 0) {
-          const float om = share[D / 2 * 64], m = fmaxf(st.m, om), safe = m == -INFINITY ? 0.f : m;
-          const float c0 = __builtin_amdgcn_exp2f(st.m - safe), c1 = __builtin_amdgcn_exp2f(om - safe);
-          st.m = m;
-          st.l = st.l * c0 + share[(D / 2 + 1) * 64] * c1;
-#pragma unroll
-          for (int b = 0; b < D / 32; b++)
-#pragma unroll
-            for (int i = 0; i < 16; i++) st.o[b][i] = st.o[b][i] * c0 + share[(b * 16 + i) * 64] * c1;
-        }
-      }
-    }
-    if (kw != 0 || !live) continue;
+    if (!live) continue;
     if (odd_values) {
       // rare: sums that such values are part of are what adding them makes of any number
 #pragma unroll 1
-      for (int pos = max(length / KEYS, g0) * KEYS; pos < min(total, g1 * KEYS); pos++) {
+      for (int pos = max(length / GRANULE, g0) * GRANULE; pos < min(total, g1 * GRANULE); pos++) {
         const int j = pos - length, page = page_at(p, seq, pos >> shift);
         const bool sees = j < 0 || (mask != nullptr ? (j >> 5) < a.mask_words && (mask[j >> 5] >> (j & 31) & 1) : j <= node);
         if (!sees || page < 0) continue;
@@ -462,7 +510,7 @@ __global__ __launch_bounds__((64 * RW * Shape<D, RW>::KW)) void tree_attention_k
 constexpr int MERGE_WAVES = 8;
 template <class T, int D, int RW>
 __global__ __launch_bounds__(64 * MERGE_WAVES) void tree_merge_kernel(TreeArgs a) {
-  constexpr int ROWS = 32 * RW, KEYS = 32 * Shape<D, RW>::KW, PER = D / 64;
+  constexpr int ROWS = 32 * RW, PER = D / 64;
   typedef float Vec __attribute__((ext_vector_type(PER)));
   typedef T VecT __attribute__((ext_vector_type(PER)));
   const pi0_pages& p = a.p;
@@ -471,8 +519,9 @@ __global__ __launch_bounds__(64 * MERGE_WAVES) void tree_merge_kernel(TreeArgs a
   const int2 rows = rows_of(a.row_start, seq, a.n_rows, a.max_rows);
   if (r >= rows.y * a.group) return;
   const int total = min(length_of(p, seq) + rows.y, p.max_pages * p.page_tokens);
-  const int granules = div_up(total, KEYS), row_tiles = div_up(rows.y * a.group, ROWS), row_tile = r / ROWS;
-  const int64_t run = a.prefix[p.n_seqs + 1], first = a.prefix[seq] + ((int64_t)kv_head * row_tiles + row_tile) * granules;
+  const int granules = div_up(total, GRANULE), row_tiles = div_up(rows.y * a.group, ROWS), row_tile = r / ROWS;
+  const Cut cut = *a.cut;
+  const int64_t run = cut.run, first = (seq > 0 ? a.upto[seq - 1] : 0) + ((int64_t)kv_head * row_tiles + row_tile) * cut.length(granules) + cut.front();
   const int b0 = (int)(first / run), b1 = (int)((first + granules - 1) / run);
   if (b0 == b1) return;
   auto slot_of = [&](int block) { return ((size_t)block * 2 + (first >= block * run)) * ROWS + r % ROWS; };
@@ -509,25 +558,26 @@ __global__ __launch_bounds__(64 * MERGE_WAVES) void tree_merge_kernel(TreeArgs a
 }
 
 struct Space {
-  size_t prefix, part_ml, bytes;   // part_o lies in front
+  size_t part_ml, upto, cut, bytes;   // part_o lies in front
 };
 template <int D, int RW>
 Space space_of(const pi0_pages& p) {
   Space s;
   const size_t slots = (size_t)Shape<D, RW>::BLOCKS * 2 * 32 * RW;
   s.part_ml = slots * D * sizeof(float);
-  s.prefix = s.part_ml + slots * sizeof(float2);
-  s.bytes = s.prefix + ((size_t)p.n_seqs + 2) * sizeof(int64_t);
+  s.upto = s.part_ml + slots * sizeof(float2);
+  s.cut = s.upto + (size_t)p.n_seqs * sizeof(int64_t);
+  s.bytes = s.cut + sizeof(Cut);
   return s;
 }
 
-// Row tiles of 32 where all rows of a sequence and key/value head fit one (single tokens, small drafts): its keys are read
-// once and the products have time to spare.  128 otherwise.
-bool few_rows(int max_rows, int group) { return max_rows * group <= 32; }
+// 32, 64 or 128 rows per tile, the least that all rows of a sequence and key/value head fit: its keys are read once then.
+int row_waves(int max_rows, int group) { return max_rows * group <= 32 ? 1 : max_rows * group <= 64 ? 2 : 4; }
 
 template <int D>
 Space space_of(const pi0_pages& p, int heads, int max_rows) {
-  return few_rows(max_rows, heads / p.kv_heads) ? space_of<D, 1>(p) : space_of<D, 4>(p);
+  const int rw = row_waves(max_rows, heads / p.kv_heads);
+  return rw == 1 ? space_of<D, 1>(p) : rw == 2 ? space_of<D, 2>(p) : space_of<D, 4>(p);
 }
 Space space_of(const pi0_pages& p, int heads, int max_rows) {
   return p.head_dim == 64 ? space_of<64>(p, heads, max_rows) : p.head_dim == 128 ? space_of<128>(p, heads, max_rows) : space_of<256>(p, heads, max_rows);
@@ -538,13 +588,16 @@ void launch(hipStream_t s, TreeArgs& a, char* ws) {
   const Space at = space_of<D, RW>(a.p);
   a.part_o = reinterpret_cast<float*>(ws);
   a.part_ml = reinterpret_cast<float2*>(ws + at.part_ml);
-  a.prefix = reinterpret_cast<int64_t*>(ws + at.prefix);
-  hipLaunchKernelGGL((tree_attention_kernel<T, D, RW>), dim3(Shape<D, RW>::BLOCKS), dim3(64 * RW * Shape<D, RW>::KW), 0, s, a);
+  a.upto = reinterpret_cast<int64_t*>(ws + at.upto);
+  a.cut = reinterpret_cast<Cut*>(ws + at.cut);
+  hipLaunchKernelGGL((tree_attention_kernel<T, D, RW>), dim3(Shape<D, RW>::BLOCKS), dim3(64 * RW), 0, s, a);
   hipLaunchKernelGGL((tree_merge_kernel<T, D, RW>), dim3(a.max_rows * a.group, a.p.kv_heads, a.p.n_seqs), dim3(64 * MERGE_WAVES), 0, s, a);
 }
 template <class T, int D>
 void launch(hipStream_t s, TreeArgs& a, char* ws) {
-  if (few_rows(a.max_rows, a.group)) launch<T, D, 1>(s, a, ws);
+  const int rw = row_waves(a.max_rows, a.group);
+  if (rw == 1) launch<T, D, 1>(s, a, ws);
+  else if (rw == 2) launch<T, D, 2>(s, a, ws);
   else launch<T, D, 4>(s, a, ws);
 }
 template <class T>
