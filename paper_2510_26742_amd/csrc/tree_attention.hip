@@ -63,15 +63,19 @@ template <> struct Shape<256, 4> { static constexpr int STAGES = 4, BLOCKS = 256
 template <> struct Shape<128, 1> { static constexpr int STAGES = 2, BLOCKS = 1024; };
 template <> struct Shape<128, 2> { static constexpr int STAGES = 4, BLOCKS = 512; };
 template <> struct Shape<128, 4> { static constexpr int STAGES = 4, BLOCKS = 512; };
+template <> struct Shape<128, 8> { static constexpr int STAGES = 4, BLOCKS = 256; };
 template <> struct Shape<64, 1> { static constexpr int STAGES = 4, BLOCKS = 1024; };
 template <> struct Shape<64, 2> { static constexpr int STAGES = 4, BLOCKS = 1024; };
 template <> struct Shape<64, 4> { static constexpr int STAGES = 4, BLOCKS = 512; };
+template <> struct Shape<64, 8> { static constexpr int STAGES = 4, BLOCKS = 512; };
 
 // Where a unit lies on the line.  length: of the unit's share of the line, front: how far behind its beginning the first granule is
 struct Cut {
-  int64_t run;
+  int run;
   int whole;   // units take up whole runs
-  __device__ __forceinline__ int64_t length(int granules) const { return whole ? (granules + run - 1) / run * run : granules > 0 ? granules + START : 0; }
+  __device__ __forceinline__ int length(int granules) const {
+    return whole ? (int)((unsigned)(granules + run - 1) / (unsigned)run) * run : granules > 0 ? granules + START : 0;
+  }
   __device__ __forceinline__ int front() const { return whole ? 0 : START; }
 };
 
@@ -91,7 +95,7 @@ struct TreeArgs {
   int near_rows;         // eight rows of a page lie within 32 bits of offsets
   int64_t layer;         // elements in front of the layer
   // workspace
-  int64_t* upto;         // [n_seqs] where a sequence's share of the line ends
+  int* upto;             // [n_seqs] where a sequence's share of the line ends
   Cut* cut;
   float* part_o;         // [blocks][2][rows of a tile][head_dim]
   float2* part_ml;       // [blocks][2][rows of a tile]: reference of the exponents, sum of the weights
@@ -126,7 +130,7 @@ __device__ __forceinline__ float dot_ones(f16x2 w, float c) { return __builtin_a
 // that decided the branch are a later product's - and the waits in front and behind cover the longest there is.
 template <int N>
 __device__ __forceinline__ void scale_sums(f32x16 (&o)[N], float c) {
-  asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
+  asm volatile("s_nop 15\n\ts_nop 15\n\ts_nop 15\n\ts_nop 15" ::: "memory");
 #pragma unroll
   for (int b = 0; b < N; b++) {
 #pragma unroll
@@ -156,100 +160,113 @@ __device__ __forceinline__ bool clean(unsigned char* at) {
   return odd;
 }
 
+// another lane's value by a data-parallel move (CTRL as the hardware counts them), 0 where there is none; ROWS: of 16 lanes that take part
+template <int CTRL, int ROWS = 0xf, class V>
+__device__ __forceinline__ V dpp(V v) {
+  return __builtin_bit_cast(V, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, ROWS, 0xf, false));
+}
+// sums over a wave's lanes, in every lane
+__device__ __forceinline__ float wave_sum(float v) {
+  v += dpp<0x111>(v);   // lanes 1, 2, 4, 8 below, inside rows of 16; then the rows' last lanes to the rows behind
+  v += dpp<0x112>(v);
+  v += dpp<0x114>(v);
+  v += dpp<0x118>(v);
+  v += dpp<0x142, 0xa>(v);
+  v += dpp<0x143, 0xc>(v);
+  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
+}
+__device__ __forceinline__ int wave_prefix(int v) {   // sum over the lanes up to this one
+  v += dpp<0x111>(v);
+  v += dpp<0x112>(v);
+  v += dpp<0x114>(v);
+  v += dpp<0x118>(v);
+  v += dpp<0x142, 0xa>(v);
+  v += dpp<0x143, 0xc>(v);
+  return v;
+}
+
 // RW waves of a block have 32 rows each and read the same tiles
 template <class T, int D, int RW>
 __global__ __launch_bounds__(64 * RW) void tree_attention_kernel(TreeArgs a) {
-  constexpr int STAGES = Shape<D, RW>::STAGES, BLOCKS = Shape<D, RW>::BLOCKS, THREADS = 64 * RW;
-  constexpr int PIECES = D / 8, TILE = 32 * D * 2, REQUESTS = TILE / 1024 / RW, KEYS_PER_REQUEST = 512 / D, ROWS = 32 * RW;
-  static_assert(REQUESTS >= 1 && STAGES >= 2 && (STAGES - 2) * 2 * REQUESTS < 64, "the wait counter holds what is in flight");
+  constexpr int STAGES = Shape<D, RW>::STAGES, BLOCKS = Shape<D, RW>::BLOCKS, ROWS = 32 * RW;
+  constexpr int PIECES = D / 8, TILE = 32 * D * 2, PARTS = TILE / 1024, REQUESTS = 2 * PARTS / RW, KEYS_PER_REQUEST = 512 / D;
+  constexpr bool AHEAD = RW >= 4;
+  constexpr int PRODUCTS = D / 16;   // of either kind, per granule
+  static_assert(REQUESTS >= 1 && STAGES >= (AHEAD ? 3 : 2) && (STAGES - 2) * REQUESTS < 64, "the wait counter holds what is in flight");
   typedef T T2 __attribute__((ext_vector_type(2)));
   typedef T T4 __attribute__((ext_vector_type(4)));
   const pi0_pages& p = a.p;
   __shared__ __align__(1024) unsigned char tiles[STAGES][2][TILE];
-  __shared__ int64_t upto[MAX_SEQS];   // where each sequence's share of the line ends
-  int64_t (*const sums)[10] = reinterpret_cast<int64_t (*)[10]>(tiles);   // before there are any tiles
+  __shared__ int upto[MAX_SEQS];   // where each sequence's share of the line ends
   const int lane = threadIdx.x & 63, rw = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
 
-  // The line: units, granules and, for nine lengths of a run, how many blocks they ask for
+  // The line, worked out by every wave for itself: lane l has the sequences l, l + 64, ..; of the first 64 it keeps what it reads
   Cut cut;
+  int my_end = 0;
+  const int2 my_rows = lane < p.n_seqs ? rows_of(a.row_start, lane, a.n_rows, a.max_rows) : int2{0, 0};
+  const int my_length = lane < p.n_seqs ? length_of(p, lane) : 0;
   {
-    const int per_thread = div_up(p.n_seqs, THREADS), s0 = threadIdx.x * per_thread, s1 = min(p.n_seqs, s0 + per_thread);
-    auto reduce = [&](int64_t (&v)[9], int n) {
-      for (int k = 0; k < n; k++) {
-        for (int i = 32; i > 0; i >>= 1) v[k] += __shfl_xor(v[k], i);
-      }
-      if constexpr (RW > 1) {
-        __syncthreads();
-        for (int k = 0; k < n; k++) {
-          if (lane == 0) sums[rw][k] = v[k];
-        }
-        __syncthreads();
-        for (int k = 0; k < n; k++) {
-          v[k] = 0;
-          for (int w = 0; w < RW; w++) v[k] += sums[w][k];
-        }
-      }
+    auto line_of = [&](int s, int* granules) {
+      const int2 rows = s == lane ? my_rows : rows_of(a.row_start, s, a.n_rows, a.max_rows);
+      const int length = s == lane ? my_length : length_of(p, s);
+      *granules = div_up(min(length + rows.y, p.max_pages * p.page_tokens), GRANULE);
+      return p.kv_heads * div_up(rows.y * a.group, ROWS);
     };
-    auto units_of = [&](int s, int* granules) {
-      const int n = rows_of(a.row_start, s, a.n_rows, a.max_rows).y;
-      *granules = div_up(min(length_of(p, s) + n, p.max_pages * p.page_tokens), GRANULE);
-      return (int64_t)p.kv_heads * div_up(n * a.group, ROWS);
-    };
-    int64_t v[9] = {};
-    for (int s = s0; s < s1; s++) {
+    float units = 0.f, total = 0.f;
+    for (int s = lane; s < p.n_seqs; s += 64) {
       int granules;
-      const int64_t units = units_of(s, &granules);
-      v[0] += units;
-      v[1] += units * granules;
-      upto[s] = units << 32 | granules;   // (its place in between; units are at most kv_heads * 1024 * 1024 / 32)
+      const int n = line_of(s, &granules);
+      units += (float)n;
+      total += (float)n * (float)granules;
     }
-    reduce(v, 2);
-    const int64_t least = max((int64_t)1, (v[1] + BLOCKS - 1) / BLOCKS);
-    cut.whole = v[0] <= BLOCKS / 2;
-    cut.run = max((int64_t)1, (v[1] + v[0] * START + BLOCKS - 1) / BLOCKS);
+    units = wave_sum(units), total = wave_sum(total);
+    cut.whole = units <= BLOCKS / 2;
+    cut.run = 1;
     if (cut.whole) {
-      for (int k = 0; k < 9; k++) v[k] = 0;
-      for (int s = s0; s < s1; s++) {
-        const int64_t units = upto[s] >> 32;
-        const int granules = (int)upto[s];
-        for (int k = 0; k < 9; k++) {
-          const unsigned run = (unsigned)(least + (least * k + 7) / 8);
-          v[k] += units * ((granules + run - 1) / run);
+      // (sums of whole numbers that matter only up to BLOCKS: exact where they decide)
+      const int least = max(1, (int)ceilf(total * (1.f / BLOCKS)));
+      float blocks[8] = {};
+      for (int s = lane; s < p.n_seqs; s += 64) {
+        int granules;
+        const int n = line_of(s, &granules);
+#pragma unroll
+        for (int k = 0; k < 8; k++) {
+          const int run = least + (least * k + 7) / 8;
+          int parts = (int)((float)granules * __builtin_amdgcn_rcpf((float)run));   // granules / run, to one or two off
+          parts += parts * run < granules;
+          parts += parts * run < granules;
+          blocks[k] += (float)n * (float)parts;
         }
       }
-      reduce(v, 9);
       cut.run = 2 * least;
+#pragma unroll
       for (int k = 7; k >= 0; k--) {
-        if (v[k] <= BLOCKS) cut.run = least + (least * k + 7) / 8;
+        if (wave_sum(blocks[k]) <= BLOCKS) cut.run = least + (least * k + 7) / 8;
       }
     }
-    int64_t mine = 0;
-    for (int s = s0; s < s1; s++) {
-      upto[s] = (upto[s] >> 32) * cut.length((int)upto[s]);
-      mine += upto[s];
+    int before = 0;
+    for (int s0 = 0; s0 < p.n_seqs; s0 += 64) {
+      const int s = s0 + lane;
+      int mine = 0;
+      if (s < p.n_seqs) {
+        int granules;
+        const int n = line_of(s, &granules);
+        mine = n * cut.length(granules);
+      }
+      const int end = before + wave_prefix(mine);
+      if (s0 == 0) my_end = end;
+      if (s < p.n_seqs) {
+        if (rw == 0) upto[s] = end;
+        if (rw == 0 && blockIdx.x == 0) a.upto[s] = end;
+      }
+      before = __builtin_amdgcn_readlane(end, 63);
     }
-    int64_t sum = mine;
-    for (int i = 1; i < 64; i <<= 1) {
-      const int64_t u = __shfl_up(sum, i);
-      if (lane >= i) sum += u;
-    }
-    if constexpr (RW > 1) {
-      if (lane == 63) sums[rw][9] = sum;
-      __syncthreads();
-      for (int w = 0; w < rw; w++) sum += sums[w][9];
-    }
-    int64_t before = sum - mine;
-    for (int s = s0; s < s1; s++) {
-      before += upto[s];
-      upto[s] = before;
-    }
-    __syncthreads();
+    if (!cut.whole) cut.run = max(1, div_up(before, BLOCKS));
+    if (blockIdx.x == 0 && threadIdx.x == 0) *a.cut = cut;
+    if (p.n_seqs > 64) __syncthreads();
   }
-  if (blockIdx.x == 0) {
-    for (int s = threadIdx.x; s < p.n_seqs; s += THREADS) a.upto[s] = upto[s];
-    if (threadIdx.x == 0) *a.cut = cut;
-  }
-  const int64_t begin = blockIdx.x * cut.run, end = min(upto[p.n_seqs - 1], begin + cut.run);
+  const int line = p.n_seqs > 64 ? upto[p.n_seqs - 1] : __builtin_amdgcn_readlane(my_end, p.n_seqs - 1);
+  const int begin = uniform((int)min((int64_t)line, (int64_t)blockIdx.x * cut.run)), end = uniform((int)min((int64_t)line, (int64_t)begin + cut.run));
 
   // This lane's pieces.  First product: key lane % 32, pieces h, h + 2, ..; second: of 4 keys and 16 d that 16 lanes read transposed,
   // key (lane % 16) / 4 and quad lane % 4.  Requests: row lane / PIECES of a KiB, its piece lane % PIECES - where the row's
@@ -262,26 +279,32 @@ __global__ __launch_bounds__(64 * RW) void tree_attention_kernel(TreeArgs a) {
   const int shift = 31 - __clz(p.page_tokens), in_page = p.page_tokens - 1;
   const unsigned lds0 = lds_address(&tiles[0][0][0]);
 
-  for (int64_t cur = begin; cur < end;) {
+  for (int cur = begin; cur < end;) {
     // the unit that this run is in
-    int seq = 0;
-    for (int top = p.n_seqs - 1; seq < top;) {
-      const int mid = (seq + top) >> 1;
-      if (upto[mid] <= cur) seq = mid + 1;
-      else top = mid;
+    int seq = 0, before, length;
+    int2 rows;
+    if (p.n_seqs <= 64) {
+      seq = __popcll(__ballot(lane < p.n_seqs && my_end <= cur));
+      before = seq > 0 ? __builtin_amdgcn_readlane(my_end, seq - 1) : 0;
+      rows.x = __builtin_amdgcn_readlane(my_rows.x, seq);
+      rows.y = __builtin_amdgcn_readlane(my_rows.y, seq);
+      length = __builtin_amdgcn_readlane(my_length, seq);
+    } else {
+      for (int top = p.n_seqs - 1; seq < top;) {
+        const int mid = (seq + top) >> 1;
+        if (upto[mid] <= cur) seq = mid + 1;
+        else top = mid;
+      }
+      seq = uniform(seq);
+      before = uniform(seq > 0 ? upto[seq - 1] : 0);
+      rows = rows_of(a.row_start, seq, a.n_rows, a.max_rows);
+      rows.x = uniform(rows.x), rows.y = uniform(rows.y);
+      length = uniform(length_of(p, seq));
     }
-    seq = uniform(seq);
-    const int64_t before = seq > 0 ? upto[seq - 1] : 0;
-    const int2 rows = rows_of(a.row_start, seq, a.n_rows, a.max_rows);
-    const int length = uniform(length_of(p, seq)), total = uniform(min(length + rows.y, p.max_pages * p.page_tokens));
-    const int granules = div_up(total, GRANULE), row_tiles = uniform(div_up(rows.y * a.group, ROWS));
-    const int64_t inside = cur - before, room = cut.length(granules);
-    int unit = (int)((double)inside / (double)room);   // right to one: the quotient is below 2^31
-    unit += inside - unit * room >= room;
-    unit = uniform(unit - (inside < unit * room));
-    const int64_t first = before + unit * room + cut.front();
-    const int g0 = uniform((int)max((int64_t)0, cur - first)), g1 = uniform((int)min((int64_t)granules, end - first));
-    const int kv_head = unit / row_tiles, row_tile = unit - kv_head * row_tiles;
+    const int total = min(length + rows.y, p.max_pages * p.page_tokens), granules = div_up(total, GRANULE), row_tiles = div_up(rows.y * a.group, ROWS);
+    const int room = cut.length(granules), unit = (unsigned)(cur - before) / (unsigned)room, first = before + unit * room + cut.front();
+    const int g0 = max(0, cur - first), g1 = min(granules, end - first);
+    const int kv_head = (unsigned)unit / (unsigned)row_tiles, row_tile = unit - kv_head * row_tiles;
     cur = before + (unit + 1) * room;
     if (g0 >= g1) continue;   // the run ends in front of the unit's first granule, or begins behind its last
 
@@ -304,30 +327,30 @@ __global__ __launch_bounds__(64 * RW) void tree_attention_kernel(TreeArgs a) {
     auto request = [&](int granule, int stage, int page0, int page1) {
       const int pos0 = granule * GRANULE;
       const unsigned to = lds0 + stage * 2 * TILE;
-      if (pos0 + 32 <= total && page0 >= 0 && page1 >= 0 && a.near_rows) {
-        const int64_t at0 = 2 * (page0 * p.page_stride + (pos0 & in_page) * p.token_stride);
-        const int64_t at1 = 2 * (page1 * p.page_stride + ((pos0 + 16) & in_page) * p.token_stride);
-        const unsigned off = my_row * (unsigned)(2 * p.token_stride);
+      const bool whole = pos0 + 32 <= total && page0 >= 0 && page1 >= 0 && a.near_rows;
+      const int64_t at0 = 2 * (page0 * p.page_stride + (pos0 & in_page) * p.token_stride);
+      const int64_t at1 = 2 * (page1 * p.page_stride + ((pos0 + 16) & in_page) * p.token_stride);
+      const unsigned off = my_row * (unsigned)(2 * p.token_stride);
+      if (whole) {
 #pragma unroll
         for (int j = 0; j < REQUESTS; j++) {
-          const int part = j * RW + rw, key0 = part * KEYS_PER_REQUEST;   // the KiB and its first key
+          const int part = (j * RW + rw) % PARTS, key0 = part * KEYS_PER_REQUEST;   // the KiB of keys or of values, and its first key
+          const bool of_v = j * RW + rw >= PARTS;
           const int64_t at = (key0 < 16 ? at0 : at1) + (key0 & 15) * (2 * p.token_stride);
-          const int turn_k = D == 64 ? (key0 >> 1) & 7 : key0 & 15, turn_v = D == 64 ? ((key0 >> 1) & 1) << 2 : (key0 & 3) << 2;
-          request_to_lds(pool_k + at, off + (piece_k0 ^ turn_k) * 16, to + part * 1024);
-          request_to_lds(pool_v + at, off + (piece_v0 ^ turn_v) * 16, to + TILE + part * 1024);
+          const int turn = D == 64 ? (of_v ? ((key0 >> 1) & 1) << 2 : (key0 >> 1) & 7) : (of_v ? (key0 & 3) << 2 : key0 & 15);
+          request_to_lds((of_v ? pool_v : pool_k) + at, off + ((of_v ? piece_v0 : piece_k0) ^ turn) * 16, to + (j * RW + rw) * 1024);
         }
       } else {
 #pragma unroll 1
         for (int j = 0; j < REQUESTS; j++) {
-          const int part = j * RW + rw, key0 = part * KEYS_PER_REQUEST;
+          const int part = (j * RW + rw) % PARTS, key0 = part * KEYS_PER_REQUEST;
+          const bool of_v = j * RW + rw >= PARTS;
           const int page = key0 < 16 ? page0 : page1, pos = pos0 + key0 + my_row;
-          const bool there = pos < total && page >= 0;
           const int64_t at = 2 * (page * p.page_stride + (pos & in_page) * p.token_stride);
-          const int turn_k = D == 64 ? (key0 >> 1) & 7 : key0 & 15, turn_v = D == 64 ? ((key0 >> 1) & 1) << 2 : (key0 & 3) << 2;
-          const char* from_k = there ? pool_k + at + (piece_k0 ^ turn_k) * 16 : reinterpret_cast<const char*>(zero_piece);
-          const char* from_v = there ? pool_v + at + (piece_v0 ^ turn_v) * 16 : reinterpret_cast<const char*>(zero_piece);
-          asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to + part * 1024), "v"(from_k) : "memory");
-          asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to + TILE + part * 1024), "v"(from_v) : "memory");
+          const int turn = D == 64 ? (of_v ? ((key0 >> 1) & 1) << 2 : (key0 >> 1) & 7) : (of_v ? (key0 & 3) << 2 : key0 & 15);
+          const char* from = (of_v ? pool_v : pool_k) + at + ((of_v ? piece_v0 : piece_k0) ^ turn) * 16;
+          if (pos >= total || page < 0) from = reinterpret_cast<const char*>(zero_piece);
+          asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to + (j * RW + rw) * 1024), "v"(from) : "memory");
         }
       }
     };
@@ -354,101 +377,147 @@ __global__ __launch_bounds__(64 * RW) void tree_attention_kernel(TreeArgs a) {
     }
     int next0 = pages[STAGES - 1][0], next1 = pages[STAGES - 1][1];
 
-    int stage = 0;
     bool odd_values = false;
-    for (int granule = g0; granule < g1; granule++) {
-      asm volatile("s_waitcnt vmcnt(%0)" ::"n"((STAGES - 2) * 2 * REQUESTS) : "memory");
-      __syncthreads();   // this granule is there, from every wave; the one before has been read by every wave
-      request(granule + STAGES - 1, stage == 0 ? STAGES - 1 : stage - 1, next0, next1);
-      none = none << 2 | (next1 < 0) << 1 | (next0 < 0);
-      next0 = page_of(granule + STAGES, 0), next1 = page_of(granule + STAGES, 1);
-      unsigned char* const tiles_v = tiles[stage][1];
-      const unsigned lds_k = lds0 + stage * 2 * TILE, lds_v = lds_k + TILE;
-      stage = stage + 1 == STAGES ? 0 : stage + 1;
-      const int pos0 = granule * GRANULE;
-
-      // A weight of zero does not silence an infinity or a NaN.  Committed values are seen by every row; drafts' values that are no
-      // numbers are taken out here and given back, below, to the rows that see them.
-      if (pos0 + GRANULE > length) {
-        bool odd = false;
-#pragma unroll
-        for (int j = 0; j < REQUESTS; j++) odd |= clean<T, false>(tiles_v + (j * RW + rw) * 1024 + lane * 16);
-        if (__syncthreads_or(odd)) {
-          odd_values = true;
-#pragma unroll
-          for (int j = 0; j < REQUESTS; j++) (void)clean<T, true>(tiles_v + (j * RW + rw) * 1024 + lane * 16);
-          __syncthreads();
-        }
+    // A weight of zero does not silence an infinity or a NaN.  Committed values are seen by every row; drafts' values that are no
+    // numbers are taken out of the tile here and given back, below, to the rows that see them.
+    auto clean_values = [&](int granule, int stage) {
+      if ((granule + 1) * GRANULE <= length) return;
+      unsigned char* const at = tiles[stage][1] + lane * 16;
+      bool odd = false;
+      for (int part = rw; part < PARTS; part += RW) odd |= clean<T, false>(at + part * 1024);
+      if (__syncthreads_or(odd)) {
+        odd_values = true;
+        for (int part = rw; part < PARTS; part += RW) (void)clean<T, true>(at + part * 1024);
+        __syncthreads();
       }
-
+    };
+    // The scores of a granule.  All of its keys' pieces are asked for first: left to itself the compiler puts a read right in front of
+    // the product that takes it, which then waits for the whole way to shared memory and back.  beside(i) goes with product i.
+    auto scores = [&](int stage, auto beside) {
+      const unsigned at = lds0 + stage * 2 * TILE;
+      s16x8 kf[PRODUCTS];
+#pragma unroll
+      for (int i = 0; i < PRODUCTS; i++) kf[i] = *((LdsPiece)(size_t)(at + (read_k ^ ((2 * i & 14) << 4))) + (2 * i & 16));
+      __builtin_amdgcn_sched_barrier(0);
       f32x16 s = {};
 #pragma unroll
-      for (int i = 0; i < D / 16; i++) {
-        const s16x8 kf = *((LdsPiece)(size_t)(lds_k + (read_k ^ ((2 * i & 14) << 4))) + (2 * i & 16));
-        s = Mat<T>::mfma(kf, q[i], s);
+      for (int i = 0; i < PRODUCTS; i++) {
+        s = Mat<T>::mfma(kf[i], q[i], s);
+        beside(i);
+        __builtin_amdgcn_sched_barrier(0);
       }
-      // what of the tile the row sees, a bit per key
-      unsigned seen = 0xffffffffu;
-      const bool drafts = pos0 + 32 > length;
-      const unsigned gone = none >> (2 * (STAGES - 1)) & 3;
-      if (drafts || gone != 0) {
-        const int j0 = pos0 - length;   // node at the tile's first key
-        if (drafts) {
-          unsigned nodes = 0;           // bit b: node max(j0, 0) + b
-          const int jn = max(j0, 0);
-          if (mask != nullptr) {
-            const int word = jn >> 5, off = jn & 31;
-            const unsigned lo = word < a.mask_words ? mask[word] : 0, hi = word + 1 < a.mask_words ? mask[word + 1] : 0;
-            nodes = (unsigned)(((unsigned long long)hi << 32 | lo) >> off);
-          } else {
-            const int visible = node - jn + 1;
-            nodes = visible >= 32 ? 0xffffffffu : visible > 0 ? (1u << visible) - 1 : 0u;
-          }
-          const int committed = min(32, max(0, -j0));
-          seen = committed >= 32 ? 0xffffffffu : (1u << committed) - 1 | nodes << committed;
-          const int have = total - pos0;
-          if (have < 32) seen &= have > 0 ? (1u << have) - 1 : 0u;
+      return s;
+    };
+    s16x8 vf[PRODUCTS];
+    auto read_values = [&](int stage, int i) {   // for product i
+      const int b = i >> 1, step = i & 1;
+      const unsigned at = lds0 + stage * 2 * TILE + TILE + (read_v ^ ((b & 3) << 6)) + (b >> 2) * 256 + step * 16 * 2 * D;
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsQuad)(size_t)at);
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsQuad)(size_t)(at + 8 * 2 * D));
+      vf[i] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    };
+    // what of a tile the row does not see becomes minus infinity.  gone: its first, last 16 keys are on no page
+    auto hide = [&](f32x16& s, int granule, unsigned gone) {
+      const int pos0 = granule * GRANULE, j0 = pos0 - length;   // node at the tile's first key
+      if (j0 + GRANULE <= 0 && gone == 0) return;
+      unsigned seen = 0xffffffffu;      // a bit per key
+      if (j0 + GRANULE > 0) {
+        unsigned nodes = 0;             // bit b: node max(j0, 0) + b
+        const int jn = max(j0, 0);
+        if (mask != nullptr) {
+          const int word = jn >> 5, off = jn & 31;
+          const unsigned lo = word < a.mask_words ? mask[word] : 0, hi = word + 1 < a.mask_words ? mask[word + 1] : 0;
+          nodes = (unsigned)(((unsigned long long)hi << 32 | lo) >> off);
+        } else {
+          const int visible = node - jn + 1;
+          nodes = visible >= 32 ? 0xffffffffu : visible > 0 ? (1u << visible) - 1 : 0u;
         }
-        if (gone & 1) seen &= 0xffff0000u;
-        if (gone & 2) seen &= 0x0000ffffu;
-        const unsigned bits = seen >> (4 * h);   // bit 8 (i / 4) + i % 4 is register i's key
-#pragma unroll
-        for (int i = 0; i < 16; i++) s[i] = bits >> (8 * (i >> 2) + (i & 3)) & 1 ? s[i] : -INFINITY;
+        const int committed = min(32, max(0, -j0));
+        seen = committed >= 32 ? 0xffffffffu : (1u << committed) - 1 | nodes << committed;
+        const int have = total - pos0;
+        if (have < 32) seen &= have > 0 ? (1u << have) - 1 : 0u;
       }
+      if (gone & 1) seen &= 0xffff0000u;
+      if (gone & 2) seen &= 0x0000ffffu;
+      const unsigned bits = seen >> (4 * h);   // bit 8 (i / 4) + i % 4 is register i's key
+#pragma unroll
+      for (int i = 0; i < 16; i++) s[i] = bits >> (8 * (i >> 2) + (i & 3)) & 1 ? s[i] : -INFINITY;
+    };
+    // The reference follows the maximum only where a weight would pass 2^(8 + HEADROOM): in the first tiles, hardly ever later.
+    // fp16 weights start at 2^HEADROOM, so that small ones keep their bits.
+    auto settle = [&](const f32x16& s) {
+      constexpr float HEADROOM = Mat<T>::EXPONENT == 0x7c00 ? 7.f : 0.f;
       float top = s[0];
 #pragma unroll
       for (int i = 1; i < 16; i++) top = fmaxf(top, s[i]);
       top = max_xor32(top) * a.scale;
-      // The reference follows the maximum only where a weight would pass 2^(8 + HEADROOM): in the first tiles, hardly ever later.
-      // fp16 weights start at 2^HEADROOM, so that small ones keep their bits.
-      constexpr float HEADROOM = sizeof(T) == 2 && Mat<T>::EXPONENT == 0x7c00 ? 7.f : 0.f;
       if (__ballot(top > st.m + (8.f + HEADROOM)) != 0) {
-        const float m = fmaxf(st.m, top - HEADROOM);
-        const float keep = st.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st.m - m);
+        const float m = fmaxf(st.m, top - HEADROOM), keep = st.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st.m - m);
         st.m = m;
         st.l *= keep;
         scale_sums<D / 32>(st.o, keep);
       }
+    };
+    s16x8 pf[2];
+    auto weigh = [&](const f32x16& s, int i) {   // registers i and i + 1
       const float m = st.m == -INFINITY ? 0.f : st.m;
-      s16x8 pf[2];
+      T2 w;
+      w[0] = (T)__builtin_amdgcn_exp2f(fmaf(s[i], a.scale, -m));
+      w[1] = (T)__builtin_amdgcn_exp2f(fmaf(s[i + 1], a.scale, -m));
+      st.l = dot_ones(w, st.l);   // of what the product takes, so that rounding a dominant weight cancels
+      pf[i >> 3][i & 7] = __builtin_bit_cast(short, (T)w[0]);
+      pf[i >> 3][(i & 7) + 1] = __builtin_bit_cast(short, (T)w[1]);
+    };
+    auto sum_values = [&]() {
 #pragma unroll
-      for (int i = 0; i < 16; i += 2) {
-        T2 w;
-        w[0] = (T)__builtin_amdgcn_exp2f(fmaf(s[i], a.scale, -m));
-        w[1] = (T)__builtin_amdgcn_exp2f(fmaf(s[i + 1], a.scale, -m));
-        st.l = dot_ones(w, st.l);   // of what the product takes, so that rounding a dominant weight cancels
-        pf[i >> 3][i & 7] = __builtin_bit_cast(short, (T)w[0]);
-        pf[i >> 3][(i & 7) + 1] = __builtin_bit_cast(short, (T)w[1]);
+      for (int i = 0; i < PRODUCTS; i++) st.o[i >> 1] = Mat<T>::mfma(vf[i], pf[i & 1], st.o[i >> 1]);
+    };
+    auto request_next = [&](int granule, int stage) {   // into the place of the stage in front of `stage`
+      none = none << 2 | (next1 < 0) << 1 | (next0 < 0);
+      request(granule + STAGES - 1, stage == 0 ? STAGES - 1 : stage - 1, next0, next1);
+    };
+    auto next_pages = [&](int granule) { next0 = page_of(granule + STAGES, 0), next1 = page_of(granule + STAGES, 1); };
+
+    int stage = 0;
+    if constexpr (AHEAD) {
+      // scores one granule ahead: their products run beside the exponentials of the granule whose values are summed next
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"((STAGES - 2) * REQUESTS) : "memory");
+      __syncthreads();
+      f32x16 s = scores(0, [](int) {});
+      hide(s, g0, none >> (2 * (STAGES - 2)) & 3);
+      settle(s);
+      for (int granule = g0; granule < g1; granule++) {
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"((STAGES - 3) * REQUESTS) : "memory");
+        __syncthreads();   // the next granule is there, from every wave; the one before this has been read by every wave
+        request_next(granule, stage);
+        clean_values(granule, stage);
+        const int stage1 = stage + 1 == STAGES ? 0 : stage + 1;
+        f32x16 s_next = scores(stage1, [&](int i) {
+          read_values(stage, i);
+#pragma unroll
+          for (int j = i * 8 / PRODUCTS; j < (i + 1) * 8 / PRODUCTS; j++) weigh(s, 2 * j);
+        });
+        sum_values();
+        hide(s_next, granule + 1, none >> (2 * (STAGES - 2)) & 3);
+        settle(s_next);
+        next_pages(granule);   // (reads that other reads would have to wait for, so: when there are none)
+        s = s_next;
+        stage = stage1;
       }
+    } else {
+      for (int granule = g0; granule < g1; granule++) {
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"((STAGES - 2) * REQUESTS) : "memory");
+        __syncthreads();   // this granule is there, from every wave; the one before has been read by every wave
+        request_next(granule, stage);
+        clean_values(granule, stage);
+        f32x16 s = scores(stage, [&](int i) { read_values(stage, i); });
+        hide(s, granule, none >> (2 * (STAGES - 1)) & 3);
+        settle(s);
 #pragma unroll
-      for (int b = 0; b < D / 32; b++) {
-#pragma unroll
-        for (int step = 0; step < 2; step++) {
-          const unsigned at = lds_v + (read_v ^ ((b & 3) << 6)) + (b >> 2) * 256 + step * 16 * 2 * D;
-          const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsQuad)(size_t)at);
-          const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsQuad)(size_t)(at + 8 * 2 * D));
-          st.o[b] = Mat<T>::mfma(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7), pf[step], st.o[b]);
-        }
+        for (int i = 0; i < 16; i += 2) weigh(s, i);
+        sum_values();
+        next_pages(granule);
+        stage = stage + 1 == STAGES ? 0 : stage + 1;
       }
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the last requests, of nothing, write to the tiles as well
@@ -505,50 +574,48 @@ __global__ __launch_bounds__(64 * RW) void tree_attention_kernel(TreeArgs a) {
   }
 }
 
-// The rows of units that several blocks had a part in: sum_z 2^(m_z - m) o_z / sum_z 2^(m_z - m) l_z, in the order of the blocks.  One
-// block per row; its 8 waves share out the parts, D / 64 numbers per lane.
-constexpr int MERGE_WAVES = 8;
-template <class T, int D, int RW>
-__global__ __launch_bounds__(64 * MERGE_WAVES) void tree_merge_kernel(TreeArgs a) {
+// The rows of units that several blocks had a part in: sum_z 2^(m_z - m) o_z / sum_z 2^(m_z - m) l_z, in the order of the blocks.  WPR
+// waves share out a row's parts, D / 64 numbers per lane: 8 where units are so few that each has many, one where they are many.
+template <class T, int D, int RW, int WPR>
+__global__ __launch_bounds__(512) void tree_merge_kernel(TreeArgs a) {
   constexpr int ROWS = 32 * RW, PER = D / 64;
   typedef float Vec __attribute__((ext_vector_type(PER)));
   typedef T VecT __attribute__((ext_vector_type(PER)));
   const pi0_pages& p = a.p;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int r = blockIdx.x, kv_head = blockIdx.y, seq = blockIdx.z;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, share = wave % WPR;
+  const int r = blockIdx.x * (8 / WPR) + wave / WPR, kv_head = blockIdx.y, seq = blockIdx.z;
   const int2 rows = rows_of(a.row_start, seq, a.n_rows, a.max_rows);
-  if (r >= rows.y * a.group) return;
+  if (r >= rows.y * a.group) return;   // (with WPR == 8 all of a block's waves)
   const int total = min(length_of(p, seq) + rows.y, p.max_pages * p.page_tokens);
   const int granules = div_up(total, GRANULE), row_tiles = div_up(rows.y * a.group, ROWS), row_tile = r / ROWS;
   const Cut cut = *a.cut;
-  const int64_t run = cut.run, first = (seq > 0 ? a.upto[seq - 1] : 0) + ((int64_t)kv_head * row_tiles + row_tile) * cut.length(granules) + cut.front();
-  const int b0 = (int)(first / run), b1 = (int)((first + granules - 1) / run);
+  const int first = (seq > 0 ? a.upto[seq - 1] : 0) + (kv_head * row_tiles + row_tile) * cut.length(granules) + cut.front();
+  const int b0 = first / cut.run, b1 = (first + granules - 1) / cut.run;
   if (b0 == b1) return;
-  auto slot_of = [&](int block) { return ((size_t)block * 2 + (first >= block * run)) * ROWS + r % ROWS; };
+  auto slot_of = [&](int block) { return ((size_t)block * 2 + (first >= block * cut.run)) * ROWS + r % ROWS; };
   float m = -INFINITY;
-  for (int b = b0 + (int)threadIdx.x; b <= b1; b += 64 * MERGE_WAVES) m = fmaxf(m, a.part_ml[slot_of(b)].x);
-  __shared__ float s_m[MERGE_WAVES], s_l[MERGE_WAVES];
-  __shared__ Vec s_o[MERGE_WAVES][64];
+  for (int b = b0 + lane; b <= b1; b += 64) m = fmaxf(m, a.part_ml[slot_of(b)].x);
   for (int i = 32; i > 0; i >>= 1) m = fmaxf(m, __shfl_xor(m, i));
-  if (lane == 0) s_m[wave] = m;
-  __syncthreads();
-  for (int w = 0; w < MERGE_WAVES; w++) m = fmaxf(m, s_m[w]);
   const float safe = m == -INFINITY ? 0.f : m;
   Vec o = {};
   float l = 0.f;
 #pragma unroll 4
-  for (int b = b0 + wave; b <= b1; b += MERGE_WAVES) {
+  for (int b = b0 + share; b <= b1; b += WPR) {
     const size_t slot = slot_of(b);
     const float2 ml = a.part_ml[slot];
     const float c = __builtin_amdgcn_exp2f(ml.x - safe);
     o += c * *reinterpret_cast<const Vec*>(a.part_o + slot * D + lane * PER);
     l += c * ml.y;
   }
-  if (lane == 0) s_l[wave] = l;
-  s_o[wave][lane] = o;
-  __syncthreads();
-  if (wave != 0) return;
-  for (int w = 1; w < MERGE_WAVES; w++) o += s_o[w][lane], l += s_l[w];
+  if constexpr (WPR > 1) {
+    __shared__ float s_l[WPR];
+    __shared__ Vec s_o[WPR][64];
+    if (lane == 0) s_l[share] = l;
+    s_o[share][lane] = o;
+    __syncthreads();
+    if (share != 0) return;
+    for (int w = 1; w < WPR; w++) o += s_o[w][lane], l += s_l[w];
+  }
   const float inv = l == 0.f ? 0.f : 1.0f / l;
   const int node = r / a.group, head = kv_head * a.group + r - node * a.group;
   VecT w;
@@ -566,18 +633,25 @@ Space space_of(const pi0_pages& p) {
   const size_t slots = (size_t)Shape<D, RW>::BLOCKS * 2 * 32 * RW;
   s.part_ml = slots * D * sizeof(float);
   s.upto = s.part_ml + slots * sizeof(float2);
-  s.cut = s.upto + (size_t)p.n_seqs * sizeof(int64_t);
+  s.cut = s.upto + (size_t)p.n_seqs * sizeof(int);
   s.bytes = s.cut + sizeof(Cut);
   return s;
 }
 
-// 32, 64 or 128 rows per tile, the least that all rows of a sequence and key/value head fit: its keys are read once then.
-int row_waves(int max_rows, int group) { return max_rows * group <= 32 ? 1 : max_rows * group <= 64 ? 2 : 4; }
+// 32, 64, 128 or 256 rows per tile, the least that all rows of a sequence and key/value head fit: its keys are read once then.
+// (256 rows of 256 d do not fit the registers of two waves per SIMD.)
+template <int D>
+constexpr int most_waves() { return D == 256 ? 4 : 8; }
+template <int D>
+int row_waves(int max_rows, int group) {
+  const int rows = max_rows * group;
+  return rows <= 32 ? 1 : rows <= 64 ? 2 : rows <= 128 ? 4 : most_waves<D>();
+}
 
 template <int D>
 Space space_of(const pi0_pages& p, int heads, int max_rows) {
-  const int rw = row_waves(max_rows, heads / p.kv_heads);
-  return rw == 1 ? space_of<D, 1>(p) : rw == 2 ? space_of<D, 2>(p) : space_of<D, 4>(p);
+  const int rw = row_waves<D>(max_rows, heads / p.kv_heads);
+  return rw == 1 ? space_of<D, 1>(p) : rw == 2 ? space_of<D, 2>(p) : rw == 4 ? space_of<D, 4>(p) : space_of<D, most_waves<D>()>(p);
 }
 Space space_of(const pi0_pages& p, int heads, int max_rows) {
   return p.head_dim == 64 ? space_of<64>(p, heads, max_rows) : p.head_dim == 128 ? space_of<128>(p, heads, max_rows) : space_of<256>(p, heads, max_rows);
@@ -588,17 +662,22 @@ void launch(hipStream_t s, TreeArgs& a, char* ws) {
   const Space at = space_of<D, RW>(a.p);
   a.part_o = reinterpret_cast<float*>(ws);
   a.part_ml = reinterpret_cast<float2*>(ws + at.part_ml);
-  a.upto = reinterpret_cast<int64_t*>(ws + at.upto);
+  a.upto = reinterpret_cast<int*>(ws + at.upto);
   a.cut = reinterpret_cast<Cut*>(ws + at.cut);
   hipLaunchKernelGGL((tree_attention_kernel<T, D, RW>), dim3(Shape<D, RW>::BLOCKS), dim3(64 * RW), 0, s, a);
-  hipLaunchKernelGGL((tree_merge_kernel<T, D, RW>), dim3(a.max_rows * a.group, a.p.kv_heads, a.p.n_seqs), dim3(64 * MERGE_WAVES), 0, s, a);
+  const int rows = a.max_rows * a.group, units = a.p.n_seqs * a.p.kv_heads * div_up(rows, 32 * RW);
+  if (units <= Shape<D, RW>::BLOCKS / 16)
+    hipLaunchKernelGGL((tree_merge_kernel<T, D, RW, 8>), dim3(rows, a.p.kv_heads, a.p.n_seqs), dim3(512), 0, s, a);
+  else
+    hipLaunchKernelGGL((tree_merge_kernel<T, D, RW, 1>), dim3(div_up(rows, 8), a.p.kv_heads, a.p.n_seqs), dim3(512), 0, s, a);
 }
 template <class T, int D>
 void launch(hipStream_t s, TreeArgs& a, char* ws) {
-  const int rw = row_waves(a.max_rows, a.group);
+  const int rw = row_waves<D>(a.max_rows, a.group);
   if (rw == 1) launch<T, D, 1>(s, a, ws);
   else if (rw == 2) launch<T, D, 2>(s, a, ws);
-  else launch<T, D, 4>(s, a, ws);
+  else if (rw == 4) launch<T, D, 4>(s, a, ws);
+  else launch<T, D, most_waves<D>()>(s, a, ws);
 }
 template <class T>
 void launch(hipStream_t s, TreeArgs& a, char* ws) {
@@ -608,8 +687,11 @@ void launch(hipStream_t s, TreeArgs& a, char* ws) {
 }
 
 bool args_ok(const pi0_pages* p, int heads, int n_rows, int max_rows) {
-  return pages_ok(p) && heads >= 1 && heads <= 1024 && heads % p->kv_heads == 0 && n_rows >= 1 && n_rows <= 1 << 24 && max_rows >= 1 &&
-         max_rows <= 1024 && max_rows <= n_rows;
+  if (!pages_ok(p) || heads < 1 || heads > 1024 || heads % p->kv_heads != 0) return false;
+  if (n_rows < 1 || n_rows > 1 << 24 || max_rows < 1 || max_rows > 1024 || max_rows > n_rows) return false;
+  // the line of all units' granules is counted in 31 bits
+  const int64_t tiles = div_up(max_rows * (heads / p->kv_heads), 32), granules = div_up(p->max_pages * p->page_tokens, GRANULE) + START;
+  return (int64_t)p->n_seqs * p->kv_heads * tiles * granules < (int64_t)1 << 30;
 }
 
 }  // namespace
