@@ -38,7 +38,7 @@ enum pi0_dtype { PI0_BF16 = 0, PI0_F16 = 1, PI0_F32 = 2 };
  *   - refs[p] counts the sequences that hold page p; 0: free.  Free pages are taken in ascending order.
  * An empty cache: table all -1, length and refs all 0.
  * Strides are in elements, multiples of 8, of the same layout for keys and values; the head_dim elements of a row are
- * contiguous.  The rows must not overlap.
+ * contiguous.  The rows must not overlap; token_stride is below 2^27.
  */
 typedef struct pi0_pages {
   void* d_k;             /* keys; 16-byte aligned                                                     */
@@ -162,7 +162,8 @@ int pi0_qk_norm_rope(const pi0_pages* pages, int layer, const pi0_rows* q, const
  *     out = sum_j softmax_j(scale * q . k_j) v_j        over what the token sees; 0 if that is nothing
  * What a token does not see does not reach it, whatever is stored there (a NaN, an unwritten page).
  *   q, out    n_rows rows of `heads` heads, a multiple of kv_heads; both of the cache's type; out may be q itself
- *   max_rows  most new tokens of a sequence, 1 .. 1024
+ *   max_rows  most new tokens of a sequence, 1 .. 1024; n_seqs * kv_heads * ceil(max_rows * heads / kv_heads / 32) *
+ *             (max_pages * page_tokens / 32 + 7) below 2^30
  *   d_mask    uint32 [n_rows][mask_words], or NULL (mask_words 0); bits behind the last word are clear
  * Products on matrix cores with fp32 sums, softmax in fp32, its weights rounded to the cache's type in front of the second
  * product.  The workspace is scratch of this call: 16-byte aligned, pi0_tree_attention_workspace_bytes

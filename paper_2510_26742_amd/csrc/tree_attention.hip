@@ -8,10 +8,11 @@
 // lane, row sums and maxima need one exchange between the two halves of a wave.  V^T is read out of row-major tiles with
 // the transposing LDS load (4 keys x 16 d per 16 lanes).
 // Tiles come straight into LDS, 16 bytes per lane; the pieces of a row are permuted by its key (on the global side: a lane
-// may fetch any piece) so that neither product's reads collide in the banks.  Keys without a page or behind the last one are
-// fetched from a piece of zeros.
+// may fetch any piece) so that neither product's reads collide in the banks. 
 #include "pages_common.h"
 #include "exec_ctx.h"
+
+#include <type_traits>
 
 namespace {
 
@@ -19,8 +20,6 @@ typedef f16 f16x2 __attribute__((ext_vector_type(2)));
 typedef f16 f16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
-
-__device__ __align__(16) unsigned char zero_piece[16];
 
 template <class T>
 struct Mat;
@@ -73,9 +72,8 @@ template <> struct Shape<64, 8> { static constexpr int STAGES = 4, BLOCKS = 512;
 struct Cut {
   int run;
   int whole;   // units take up whole runs
-  __device__ __forceinline__ int length(int granules) const {
-    return whole ? (int)((unsigned)(granules + run - 1) / (unsigned)run) * run : granules > 0 ? granules + START : 0;
-  }
+  __device__ __forceinline__ int parts(int granules) const { return (int)((unsigned)(granules + run - 1) / (unsigned)run); }
+  __device__ __forceinline__ int length(int granules) const { return whole ? parts(granules) * run : granules > 0 ? granules + START : 0; }
   __device__ __forceinline__ int front() const { return whole ? 0 : START; }
 };
 
@@ -89,10 +87,9 @@ struct TreeArgs {
   int n_rows, max_rows;
   const unsigned* mask;
   int mask_words;
-  float scale;           // times log2(e), >= 0
-  short negate;          // 0x8000 where the queries' signs are turned instead of the scale's
-  short q_bits;          // 0 where the queries are taken as zero (scale 0)
-  int near_rows;         // eight rows of a page lie within 32 bits of offsets
+  float scale;           // times log2(e), > 0
+  int odd_scale;         // it was not: the queries' signs are turned (negate) or all of their bits cleared (q_bits)
+  short negate, q_bits;
   int64_t layer;         // elements in front of the layer
   // workspace
   int* upto;             // [n_seqs] where a sequence's share of the line ends
@@ -197,76 +194,64 @@ __global__ __launch_bounds__(64 * RW) void tree_attention_kernel(TreeArgs a) {
   typedef T T4 __attribute__((ext_vector_type(4)));
   const pi0_pages& p = a.p;
   __shared__ __align__(1024) unsigned char tiles[STAGES][2][TILE];
-  __shared__ int upto[MAX_SEQS];   // where each sequence's share of the line ends
+  __shared__ int2 line_of[MAX_SEQS];   // units and granules of a sequence, then where its share of the line ends (x)
   const int lane = threadIdx.x & 63, rw = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
 
-  // The line, worked out by every wave for itself: lane l has the sequences l, l + 64, ..; of the first 64 it keeps what it reads
+  // The line, worked out by every wave for itself: lane l has the sequences l, l + 64, ..; what it knows of the first 64 stays in
+  // registers.  (Whatever runs once per block is written to be short: a block starts with its code far away, and 64 bytes
+  // of it cost about as long as a read of memory that is near.)
   Cut cut;
-  int my_end = 0;
-  const int2 my_rows = lane < p.n_seqs ? rows_of(a.row_start, lane, a.n_rows, a.max_rows) : int2{0, 0};
-  const int my_length = lane < p.n_seqs ? length_of(p, lane) : 0;
+  int line, my_end = 0;
+  int2 my_rows = {0, 0}, mine = {0, 0};
+  int my_length = 0;
   {
-    auto line_of = [&](int s, int* granules) {
-      const int2 rows = s == lane ? my_rows : rows_of(a.row_start, s, a.n_rows, a.max_rows);
-      const int length = s == lane ? my_length : length_of(p, s);
-      *granules = div_up(min(length + rows.y, p.max_pages * p.page_tokens), GRANULE);
-      return p.kv_heads * div_up(rows.y * a.group, ROWS);
-    };
     float units = 0.f, total = 0.f;
+#pragma unroll 1
     for (int s = lane; s < p.n_seqs; s += 64) {
-      int granules;
-      const int n = line_of(s, &granules);
-      units += (float)n;
-      total += (float)n * (float)granules;
+      const int2 rows = rows_of(a.row_start, s, a.n_rows, a.max_rows);
+      const int length = length_of(p, s);
+      const int2 here = {p.kv_heads * div_up(rows.y * a.group, ROWS), div_up(min(length + rows.y, p.max_pages * p.page_tokens), GRANULE)};
+      if (s == lane) my_rows = rows, my_length = length, mine = here;
+      else line_of[s] = here;   // (each wave the same, and a lane reads only what it has written itself)
+      units += (float)here.x;
+      total += (float)here.x * (float)here.y;
     }
     units = wave_sum(units), total = wave_sum(total);
     cut.whole = units <= BLOCKS / 2;
-    cut.run = 1;
+    cut.run = max(1, (int)ceilf(total * (1.f / BLOCKS)));
     if (cut.whole) {
-      // (sums of whole numbers that matter only up to BLOCKS: exact where they decide)
-      const int least = max(1, (int)ceilf(total * (1.f / BLOCKS)));
-      float blocks[8] = {};
-      for (int s = lane; s < p.n_seqs; s += 64) {
-        int granules;
-        const int n = line_of(s, &granules);
-#pragma unroll
-        for (int k = 0; k < 8; k++) {
-          const int run = least + (least * k + 7) / 8;
-          int parts = (int)((float)granules * __builtin_amdgcn_rcpf((float)run));   // granules / run, to one or two off
-          parts += parts * run < granules;
-          parts += parts * run < granules;
-          blocks[k] += (float)n * (float)parts;
+      // (sums of whole numbers that matter only up to BLOCKS: exact where they decide.  Ends with one part per unit at the latest)
+      const int more = cut.run / 8 + 1;
+#pragma unroll 1
+      for (;; cut.run += more) {
+        float blocks = 0.f;
+#pragma unroll 1
+        for (int s = lane; s < p.n_seqs; s += 64) {
+          const int2 here = s == lane ? mine : line_of[s];
+          blocks += (float)here.x * (float)cut.parts(here.y);
         }
-      }
-      cut.run = 2 * least;
-#pragma unroll
-      for (int k = 7; k >= 0; k--) {
-        if (wave_sum(blocks[k]) <= BLOCKS) cut.run = least + (least * k + 7) / 8;
+        if (wave_sum(blocks) <= BLOCKS) break;
       }
     }
     int before = 0;
+#pragma unroll 1
     for (int s0 = 0; s0 < p.n_seqs; s0 += 64) {
       const int s = s0 + lane;
-      int mine = 0;
-      if (s < p.n_seqs) {
-        int granules;
-        const int n = line_of(s, &granules);
-        mine = n * cut.length(granules);
-      }
-      const int end = before + wave_prefix(mine);
+      const int2 here = s0 == 0 ? mine : s < p.n_seqs ? line_of[s] : int2{0, 0};
+      const int end = before + wave_prefix(here.x * cut.length(here.y));
       if (s0 == 0) my_end = end;
-      if (s < p.n_seqs) {
-        if (rw == 0) upto[s] = end;
-        if (rw == 0 && blockIdx.x == 0) a.upto[s] = end;
+      if (rw == 0 && s < p.n_seqs) {
+        line_of[s].x = end;
+        if (blockIdx.x == 0) a.upto[s] = end;
       }
       before = __builtin_amdgcn_readlane(end, 63);
     }
-    if (!cut.whole) cut.run = max(1, div_up(before, BLOCKS));
+    line = before;
+    if (!cut.whole) cut.run = max(1, div_up(line, BLOCKS));
     if (blockIdx.x == 0 && threadIdx.x == 0) *a.cut = cut;
     if (p.n_seqs > 64) __syncthreads();
   }
-  const int line = p.n_seqs > 64 ? upto[p.n_seqs - 1] : __builtin_amdgcn_readlane(my_end, p.n_seqs - 1);
-  const int begin = uniform((int)min((int64_t)line, (int64_t)blockIdx.x * cut.run)), end = uniform((int)min((int64_t)line, (int64_t)begin + cut.run));
+  const int begin = (int)min((int64_t)line, (int64_t)blockIdx.x * cut.run), end = (int)min((int64_t)line, (int64_t)begin + cut.run);
 
   // This lane's pieces.  First product: key lane % 32, pieces h, h + 2, ..; second: of 4 keys and 16 d that 16 lanes read transposed,
   // key (lane % 16) / 4 and quad lane % 4.  Requests: row lane / PIECES of a KiB, its piece lane % PIECES - where the row's
@@ -292,11 +277,11 @@ __global__ __launch_bounds__(64 * RW) void tree_attention_kernel(TreeArgs a) {
     } else {
       for (int top = p.n_seqs - 1; seq < top;) {
         const int mid = (seq + top) >> 1;
-        if (upto[mid] <= cur) seq = mid + 1;
+        if (line_of[mid].x <= cur) seq = mid + 1;
         else top = mid;
       }
       seq = uniform(seq);
-      before = uniform(seq > 0 ? upto[seq - 1] : 0);
+      before = uniform(seq > 0 ? line_of[seq - 1].x : 0);
       rows = rows_of(a.row_start, seq, a.n_rows, a.max_rows);
       rows.x = uniform(rows.x), rows.y = uniform(rows.y);
       length = uniform(length_of(p, seq));
@@ -304,59 +289,47 @@ __global__ __launch_bounds__(64 * RW) void tree_attention_kernel(TreeArgs a) {
     const int total = min(length + rows.y, p.max_pages * p.page_tokens), granules = div_up(total, GRANULE), row_tiles = div_up(rows.y * a.group, ROWS);
     const int room = cut.length(granules), unit = (unsigned)(cur - before) / (unsigned)room, first = before + unit * room + cut.front();
     const int g0 = max(0, cur - first), g1 = min(granules, end - first);
-    const int kv_head = (unsigned)unit / (unsigned)row_tiles, row_tile = unit - kv_head * row_tiles;
+    int kv_head = unit;
+    if (row_tiles > 1) kv_head = (unsigned)unit / (unsigned)row_tiles;
+    const int row_tile = unit - kv_head * row_tiles;
     cur = before + (unit + 1) * room;
     if (g0 >= g1) continue;   // the run ends in front of the unit's first granule, or begins behind its last
 
     // this lane's row: token and head
     const int r = row_tile * ROWS + rw * 32 + (lane & 31);
     const bool live = r < rows.y * a.group;
-    const int node = live ? r / a.group : 0, head = kv_head * a.group + (live ? r - node * a.group : 0);
+    // r / group: both below 2^20, and half a row is more than the reciprocal is off by
+    const int node = live ? (int)(((float)r + 0.5f) * __builtin_amdgcn_rcpf((float)a.group)) : 0, head = kv_head * a.group + (live ? r - node * a.group : 0);
     s16x8 q[D / 16];   // (a lane without a row takes the tile's first token's, and gives nothing back)
     const T* const q_row = reinterpret_cast<const T*>(a.q) + (rows.x + node) * a.q_row_stride + head * a.q_head_stride + h * 8;
 #pragma unroll
     for (int i = 0; i < D / 16; i++) q[i] = *reinterpret_cast<const s16x8*>(q_row + i * 16);
+    if (a.odd_scale) {
 #pragma unroll
-    for (int i = 0; i < D / 16; i++) q[i] = (q[i] ^ a.negate) & a.q_bits;
+      for (int i = 0; i < D / 16; i++) q[i] = (q[i] ^ a.negate) & a.q_bits;
+    }
     const unsigned* mask = a.mask != nullptr ? a.mask + (size_t)(rows.x + node) * a.mask_words : nullptr;
     const char* const pool_k = reinterpret_cast<const char*>(p.d_k) + 2 * (a.layer + kv_head * p.head_stride);
     const char* const pool_v = reinterpret_cast<const char*>(p.d_v) + 2 * (a.layer + kv_head * p.head_stride);
 
-    // Requests this wave's part of a granule, of whose keys the first and last 16 lie in pages page0 and page1 (-1: none; a granule
-    // behind the last is asked for as well, as zeros, so that as many requests are in flight at the end as anywhere).
+    // Requests this wave's part of a granule, of whose keys the first and last 16 lie in pages page0 and page1.  Where there is no page
+    // (-1), and behind the last position, some row is read that the scores then hide.
     auto request = [&](int granule, int stage, int page0, int page1) {
       const int pos0 = granule * GRANULE;
-      const unsigned to = lds0 + stage * 2 * TILE;
-      const bool whole = pos0 + 32 <= total && page0 >= 0 && page1 >= 0 && a.near_rows;
-      const int64_t at0 = 2 * (page0 * p.page_stride + (pos0 & in_page) * p.token_stride);
-      const int64_t at1 = 2 * (page1 * p.page_stride + ((pos0 + 16) & in_page) * p.token_stride);
-      const unsigned off = my_row * (unsigned)(2 * p.token_stride);
-      if (whole) {
+      const unsigned to = lds0 + stage * 2 * TILE, off = my_row * (unsigned)(2 * p.token_stride);
+      const int64_t at0 = 2 * (max(page0, 0) * p.page_stride + (pos0 & in_page) * p.token_stride);
+      const int64_t at1 = 2 * (max(page1, 0) * p.page_stride + ((pos0 + 16) & in_page) * p.token_stride);
 #pragma unroll
-        for (int j = 0; j < REQUESTS; j++) {
-          const int part = (j * RW + rw) % PARTS, key0 = part * KEYS_PER_REQUEST;   // the KiB of keys or of values, and its first key
-          const bool of_v = j * RW + rw >= PARTS;
-          const int64_t at = (key0 < 16 ? at0 : at1) + (key0 & 15) * (2 * p.token_stride);
-          const int turn = D == 64 ? (of_v ? ((key0 >> 1) & 1) << 2 : (key0 >> 1) & 7) : (of_v ? (key0 & 3) << 2 : key0 & 15);
-          request_to_lds((of_v ? pool_v : pool_k) + at, off + ((of_v ? piece_v0 : piece_k0) ^ turn) * 16, to + (j * RW + rw) * 1024);
-        }
-      } else {
-#pragma unroll 1
-        for (int j = 0; j < REQUESTS; j++) {
-          const int part = (j * RW + rw) % PARTS, key0 = part * KEYS_PER_REQUEST;
-          const bool of_v = j * RW + rw >= PARTS;
-          const int page = key0 < 16 ? page0 : page1, pos = pos0 + key0 + my_row;
-          const int64_t at = 2 * (page * p.page_stride + (pos & in_page) * p.token_stride);
-          const int turn = D == 64 ? (of_v ? ((key0 >> 1) & 1) << 2 : (key0 >> 1) & 7) : (of_v ? (key0 & 3) << 2 : key0 & 15);
-          const char* from = (of_v ? pool_v : pool_k) + at + ((of_v ? piece_v0 : piece_k0) ^ turn) * 16;
-          if (pos >= total || page < 0) from = reinterpret_cast<const char*>(zero_piece);
-          asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to + (j * RW + rw) * 1024), "v"(from) : "memory");
-        }
+      for (int j = 0; j < REQUESTS; j++) {
+        const int part = (j * RW + rw) % PARTS, key0 = part * KEYS_PER_REQUEST;   // the KiB of keys or of values, and its first key
+        const bool of_v = j * RW + rw >= PARTS;
+        const int64_t at = (key0 < 16 ? at0 : at1) + (key0 & 15) * (2 * p.token_stride);
+        const int turn = D == 64 ? (of_v ? ((key0 >> 1) & 1) << 2 : (key0 >> 1) & 7) : (of_v ? (key0 & 3) << 2 : key0 & 15);
+        request_to_lds((of_v ? pool_v : pool_k) + at, off + ((of_v ? piece_v0 : piece_k0) ^ turn) * 16, to + (j * RW + rw) * 1024);
       }
     };
     auto page_of = [&](int granule, int half) {
-      const int page = uniform_page(p, seq, (granule * GRANULE + half * 16) >> shift);
-      return granule < g1 ? page : -1;
+      return uniform_page(p, seq, (granule * GRANULE + half * 16) >> shift);
     };
 
     RowState<D> st;
@@ -365,7 +338,7 @@ __global__ __launch_bounds__(64 * RW) void tree_attention_kernel(TreeArgs a) {
     st.m = -INFINITY;
     st.l = 0.f;
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // from here on only the tiles' requests are in flight
-    __syncthreads();                                   // what was in the tiles has been read, and nothing is on its way there
+    __syncthreads();                                   // what was in the tiles has been read
     unsigned none = 0;   // two bits per granule, the latest requested lowest: its first, last 16 keys are on no page
     int pages[STAGES][2];
 #pragma unroll
@@ -373,20 +346,20 @@ __global__ __launch_bounds__(64 * RW) void tree_attention_kernel(TreeArgs a) {
 #pragma unroll
     for (int i = 0; i < STAGES - 1; i++) {
       none = none << 2 | (pages[i][1] < 0) << 1 | (pages[i][0] < 0);
-      request(g0 + i, i, pages[i][0], pages[i][1]);
+      if (g0 + i < g1) request(g0 + i, i, pages[i][0], pages[i][1]);
     }
     int next0 = pages[STAGES - 1][0], next1 = pages[STAGES - 1][1];
 
-    bool odd_values = false;
-    // A weight of zero does not silence an infinity or a NaN.  Committed values are seen by every row; drafts' values that are no
-    // numbers are taken out of the tile here and given back, below, to the rows that see them.
-    auto clean_values = [&](int granule, int stage) {
-      if ((granule + 1) * GRANULE <= length) return;
+    int odd_from = g1;   // first granule with such values
+    // A weight of zero does not silence an infinity or a NaN.  Committed values are seen by every row; where there is anything
+    // that a row may not see, values that are no numbers are taken out of the tile here and given back, below, to the rows that see them.
+    auto clean_values = [&](int granule, int stage, unsigned gone) {
+      if ((granule + 1) * GRANULE <= length && gone == 0) return;
       unsigned char* const at = tiles[stage][1] + lane * 16;
       bool odd = false;
       for (int part = rw; part < PARTS; part += RW) odd |= clean<T, false>(at + part * 1024);
-      if (__syncthreads_or(odd)) {
-        odd_values = true;
+      if (RW > 1 ? __syncthreads_or(odd) : __ballot(odd) != 0) {
+        odd_from = min(odd_from, granule);
         for (int part = rw; part < PARTS; part += RW) (void)clean<T, true>(at + part * 1024);
         __syncthreads();
       }
@@ -474,23 +447,27 @@ __global__ __launch_bounds__(64 * RW) void tree_attention_kernel(TreeArgs a) {
     };
     auto request_next = [&](int granule, int stage) {   // into the place of the stage in front of `stage`
       none = none << 2 | (next1 < 0) << 1 | (next0 < 0);
-      request(granule + STAGES - 1, stage == 0 ? STAGES - 1 : stage - 1, next0, next1);
+      if (granule + STAGES - 1 < g1) request(granule + STAGES - 1, stage == 0 ? STAGES - 1 : stage - 1, next0, next1);
+    };
+    // until a granule is there: AFTER granules behind it may be on their way, and all are waited for where the unit has fewer
+    auto arrived = [&](int granule, auto after) {
+      if (granule + after < g1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(after * REQUESTS) : "memory");
+      else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      __syncthreads();   // from every wave; and the granule before has been read by every wave
     };
     auto next_pages = [&](int granule) { next0 = page_of(granule + STAGES, 0), next1 = page_of(granule + STAGES, 1); };
 
     int stage = 0;
     if constexpr (AHEAD) {
       // scores one granule ahead: their products run beside the exponentials of the granule whose values are summed next
-      asm volatile("s_waitcnt vmcnt(%0)" ::"n"((STAGES - 2) * REQUESTS) : "memory");
-      __syncthreads();
+      arrived(g0, std::integral_constant<int, STAGES - 2>());
       f32x16 s = scores(0, [](int) {});
       hide(s, g0, none >> (2 * (STAGES - 2)) & 3);
       settle(s);
       for (int granule = g0; granule < g1; granule++) {
-        asm volatile("s_waitcnt vmcnt(%0)" ::"n"((STAGES - 3) * REQUESTS) : "memory");
-        __syncthreads();   // the next granule is there, from every wave; the one before this has been read by every wave
+        arrived(granule + 1, std::integral_constant<int, STAGES - 3>());
         request_next(granule, stage);
-        clean_values(granule, stage);
+        clean_values(granule, stage, none >> (2 * (STAGES - 1)) & 3);
         const int stage1 = stage + 1 == STAGES ? 0 : stage + 1;
         f32x16 s_next = scores(stage1, [&](int i) {
           read_values(stage, i);
@@ -498,18 +475,19 @@ __global__ __launch_bounds__(64 * RW) void tree_attention_kernel(TreeArgs a) {
           for (int j = i * 8 / PRODUCTS; j < (i + 1) * 8 / PRODUCTS; j++) weigh(s, 2 * j);
         });
         sum_values();
-        hide(s_next, granule + 1, none >> (2 * (STAGES - 2)) & 3);
-        settle(s_next);
+        if (granule + 1 < g1) {
+          hide(s_next, granule + 1, none >> (2 * (STAGES - 2)) & 3);
+          settle(s_next);
+        }
         next_pages(granule);   // (reads that other reads would have to wait for, so: when there are none)
         s = s_next;
         stage = stage1;
       }
     } else {
       for (int granule = g0; granule < g1; granule++) {
-        asm volatile("s_waitcnt vmcnt(%0)" ::"n"((STAGES - 2) * REQUESTS) : "memory");
-        __syncthreads();   // this granule is there, from every wave; the one before has been read by every wave
+        arrived(granule, std::integral_constant<int, STAGES - 2>());
         request_next(granule, stage);
-        clean_values(granule, stage);
+        clean_values(granule, stage, none >> (2 * (STAGES - 1)) & 3);
         f32x16 s = scores(stage, [&](int i) { read_values(stage, i); });
         hide(s, granule, none >> (2 * (STAGES - 1)) & 3);
         settle(s);
@@ -520,14 +498,13 @@ __global__ __launch_bounds__(64 * RW) void tree_attention_kernel(TreeArgs a) {
         stage = stage + 1 == STAGES ? 0 : stage + 1;
       }
     }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the last requests, of nothing, write to the tiles as well
     st.l = add_xor32(st.l);
 
     if (!live) continue;
-    if (odd_values) {
+    if (odd_from < g1) {
       // rare: sums that such values are part of are what adding them makes of any number
 #pragma unroll 1
-      for (int pos = max(length / GRANULE, g0) * GRANULE; pos < min(total, g1 * GRANULE); pos++) {
+      for (int pos = odd_from * GRANULE; pos < min(total, g1 * GRANULE); pos++) {
         const int j = pos - length, page = page_at(p, seq, pos >> shift);
         const bool sees = j < 0 || (mask != nullptr ? (j >> 5) < a.mask_words && (mask[j >> 5] >> (j & 31) & 1) : j <= node);
         if (!sees || page < 0) continue;
@@ -725,13 +702,13 @@ int pi0_tree_attention(const pi0_pages* pages, int layer, const pi0_rows* q, con
   a.mask = d_mask;
   a.mask_words = mask_words;
   a.scale = fabsf(scale) * 1.4426950408889634f;
+  a.odd_scale = !(scale > 0.f);
   a.negate = scale < 0.f ? (short)0x8000 : 0;
   a.q_bits = -1;
   if (a.scale == 0.f) {   // all scores are zero, and a masked one stays minus infinity
     a.q_bits = 0;
     a.scale = 1.f;
   }
-  a.near_rows = pages->token_stride < (int64_t)1 << 27;
   a.layer = layer * pages->layer_stride;
   hipStream_t s = reinterpret_cast<hipStream_t>(hip_stream);
   if (pages->dtype == PI0_BF16) launch<bf16>(s, a, reinterpret_cast<char*>(d_workspace));
