@@ -41,14 +41,15 @@ struct Mat<f16> {
 
 // How the work is cut.  A unit is a tile of 32 RW rows of one sequence and key/value head against all of its keys, in granules of 32
 // keys.  Lengths differ, and the host does not know them, so every block works out from the lengths which granules are its
-// own: the units lie behind each other in the order (sequence, head, row tile) on a line that is cut into runs of equal length,
-// one per block.
+// own: the units lie behind each other on a line that is cut into runs of equal length, one per block.
 //   - Few units (at most half as many as blocks): each takes up a whole number of runs, so that a block has part of one unit
-//     only; the shortest run for which there are blocks enough, of nine between the least and twice that.
+//     only; the shortest run, in steps of an eighth, for which there are blocks enough.  The row tiles of a head lie side by side, part
+//     by part, and neighbouring runs go to blocks of one die: its L2 gives the same keys to all of them (8 x 64 nodes over
+//     16384, four tiles of 128 rows: TODO us, with the tiles behind each other 45).
 //   - Many: the line is dense, except that a unit is START granules longer than it is - what a block spends before a unit's
 //     first granule and behind its last -, and a run may end one unit, hold others and begin the next.
-// A block writes a unit that it has all of; of any other it leaves a partial result, in slot 0 if its run begins inside of the
-// unit, in slot 1 if the unit begins inside the run, and the second launch joins them.
+// A block writes a unit that it has all of; of any other it leaves a partial result, in slot 1 if it has the first granule, in slot 0
+// if not, and the second launch joins them.
 constexpr int GRANULE = 32, START = 6;
 
 // A stage of K and V tiles is 128 D bytes; STAGES of them per block.  With one row tile per wave and 256 d the registers hold one
@@ -74,7 +75,6 @@ struct Cut {
   int whole;   // units take up whole runs
   __device__ __forceinline__ int parts(int granules) const { return (int)((unsigned)(granules + run - 1) / (unsigned)run); }
   __device__ __forceinline__ int length(int granules) const { return whole ? parts(granules) * run : granules > 0 ? granules + START : 0; }
-  __device__ __forceinline__ int front() const { return whole ? 0 : START; }
 };
 
 struct TreeArgs {
@@ -94,8 +94,8 @@ struct TreeArgs {
   // workspace
   int* upto;             // [n_seqs] where a sequence's share of the line ends
   Cut* cut;
-  float* part_o;         // [blocks][2][rows of a tile][head_dim]
-  float2* part_ml;       // [blocks][2][rows of a tile]: reference of the exponents, sum of the weights
+  float* part_o;         // [runs][2][rows of a tile][head_dim]
+  float2* part_ml;       // [runs][2][rows of a tile]: reference of the exponents, sum of the weights
 };
 
 // page_at for a sequence and entry that are the same for the whole wave: through the scalar cache, so that it does not
@@ -251,7 +251,9 @@ __global__ __launch_bounds__(64 * RW) void tree_attention_kernel(TreeArgs a) {
     if (blockIdx.x == 0 && threadIdx.x == 0) *a.cut = cut;
     if (p.n_seqs > 64) __syncthreads();
   }
-  const int begin = (int)min((int64_t)line, (int64_t)blockIdx.x * cut.run), end = (int)min((int64_t)line, (int64_t)begin + cut.run);
+  // blocks go to the chip's eight dies in turn
+  const int mine_run = (blockIdx.x & 7) * (BLOCKS / 8) + (blockIdx.x >> 3);
+  const int begin = (int)min((int64_t)line, (int64_t)mine_run * cut.run), end = (int)min((int64_t)line, (int64_t)begin + cut.run);
 
   // This lane's pieces.  First product: key lane % 32, pieces h, h + 2, ..; second: of 4 keys and 16 d that 16 lanes read transposed,
   // key (lane % 16) / 4 and quad lane % 4.  Requests: row lane / PIECES of a KiB, its piece lane % PIECES - where the row's
@@ -287,13 +289,21 @@ __global__ __launch_bounds__(64 * RW) void tree_attention_kernel(TreeArgs a) {
       length = uniform(length_of(p, seq));
     }
     const int total = min(length + rows.y, p.max_pages * p.page_tokens), granules = div_up(total, GRANULE), row_tiles = div_up(rows.y * a.group, ROWS);
-    const int room = cut.length(granules), unit = (unsigned)(cur - before) / (unsigned)room, first = before + unit * room + cut.front();
-    const int g0 = max(0, cur - first), g1 = min(granules, end - first);
-    int kv_head = unit;
-    if (row_tiles > 1) kv_head = (unsigned)unit / (unsigned)row_tiles;
-    const int row_tile = unit - kv_head * row_tiles;
-    cur = before + (unit + 1) * room;
-    if (g0 >= g1) continue;   // the run ends in front of the unit's first granule, or begins behind its last
+    const int inside = cur - before, room = cut.length(granules) * row_tiles;   // of a key/value head
+    const int kv_head = p.kv_heads > 1 ? (unsigned)inside / (unsigned)room : 0, in_head = inside - kv_head * room;
+    int row_tile, g0, g1;
+    if (cut.whole) {
+      const int chunk = (unsigned)in_head / (unsigned)cut.run, part = row_tiles > 1 ? (unsigned)chunk / (unsigned)row_tiles : chunk;
+      row_tile = chunk - part * row_tiles;
+      g0 = part * cut.run, g1 = min(granules, g0 + cut.run);
+      cur = end;
+    } else {
+      row_tile = row_tiles > 1 ? (unsigned)in_head / (unsigned)(granules + START) : 0;
+      const int first = before + kv_head * room + row_tile * (granules + START) + START;
+      g0 = max(0, cur - first), g1 = min(granules, end - first);
+      cur = first + granules;
+      if (g0 >= g1) continue;   // the run ends in front of the unit's first granule
+    }
 
     // this lane's row: token and head
     const int r = row_tile * ROWS + rw * 32 + (lane & 31);
@@ -313,19 +323,27 @@ __global__ __launch_bounds__(64 * RW) void tree_attention_kernel(TreeArgs a) {
     const char* const pool_v = reinterpret_cast<const char*>(p.d_v) + 2 * (a.layer + kv_head * p.head_stride);
 
     // Requests this wave's part of a granule, of whose keys the first and last 16 lie in pages page0 and page1.  Where there is no page
-    // (-1), and behind the last position, some row is read that the scores then hide.
+    // (-1), and behind the last position, some row is read that the scores then hide.  A quarter of a granule is 16 keys, or the
+    // values of 16; a wave has several quarters, one, or half of one.
+    constexpr int QUARTER = PARTS / 2, SHARE = RW > 4 ? QUARTER / (RW / 4) : QUARTER;   // KiB
     auto request = [&](int granule, int stage, int page0, int page1) {
       const int pos0 = granule * GRANULE;
-      const unsigned to = lds0 + stage * 2 * TILE, off = my_row * (unsigned)(2 * p.token_stride);
+      const unsigned off = my_row * (unsigned)(2 * p.token_stride), to = lds0 + stage * 2 * TILE;
       const int64_t at0 = 2 * (max(page0, 0) * p.page_stride + (pos0 & in_page) * p.token_stride);
       const int64_t at1 = 2 * (max(page1, 0) * p.page_stride + ((pos0 + 16) & in_page) * p.token_stride);
+#pragma unroll 1
+      for (int quarter = RW > 4 ? rw / (RW / 4) : rw; quarter < 4; quarter += RW) {
+        const bool of_v = quarter >= 2;
+        const int kib0 = RW > 4 ? rw % (RW / 4) * SHARE : 0;
+        const char* const from = (of_v ? pool_v : pool_k) + (quarter & 1 ? at1 : at0);
+        const int piece0 = of_v ? piece_v0 : piece_k0;
 #pragma unroll
-      for (int j = 0; j < REQUESTS; j++) {
-        const int part = (j * RW + rw) % PARTS, key0 = part * KEYS_PER_REQUEST;   // the KiB of keys or of values, and its first key
-        const bool of_v = j * RW + rw >= PARTS;
-        const int64_t at = (key0 < 16 ? at0 : at1) + (key0 & 15) * (2 * p.token_stride);
-        const int turn = D == 64 ? (of_v ? ((key0 >> 1) & 1) << 2 : (key0 >> 1) & 7) : (of_v ? (key0 & 3) << 2 : key0 & 15);
-        request_to_lds((of_v ? pool_v : pool_k) + at, off + ((of_v ? piece_v0 : piece_k0) ^ turn) * 16, to + (j * RW + rw) * 1024);
+        for (int j = 0; j < SHARE; j++) {
+          const int kib = kib0 + j, key = kib * KEYS_PER_REQUEST;   // of the quarter, and its first key
+          // key's bits that turn the pieces; of a value's, only those that are not the same for the whole quarter
+          const int turn_k = D == 64 ? ((quarter & 1) * 16 + key) >> 1 & 7 : key, turn_v = D == 64 ? (key >> 1 & 1) << 2 : (key & 3) << 2;
+          request_to_lds(from + key * (2 * p.token_stride), off + (piece0 ^ (of_v ? turn_v : turn_k)) * 16, to + (quarter * QUARTER + kib) * 1024);
+        }
       }
     };
     auto page_of = [&](int granule, int half) {
@@ -365,13 +383,15 @@ __global__ __launch_bounds__(64 * RW) void tree_attention_kernel(TreeArgs a) {
       }
     };
     // The scores of a granule.  All of its keys' pieces are asked for first: left to itself the compiler puts a read right in front of
-    // the product that takes it, which then waits for the whole way to shared memory and back.  beside(i) goes with product i.
-    auto scores = [&](int stage, auto beside) {
+    // the product that takes it, which then waits for the whole way to shared memory and back.  meanwhile() is done on that way,
+    // beside(i) goes with product i.
+    auto scores = [&](int stage, auto meanwhile, auto beside) {
       const unsigned at = lds0 + stage * 2 * TILE;
       s16x8 kf[PRODUCTS];
 #pragma unroll
       for (int i = 0; i < PRODUCTS; i++) kf[i] = *((LdsPiece)(size_t)(at + (read_k ^ ((2 * i & 14) << 4))) + (2 * i & 16));
       __builtin_amdgcn_sched_barrier(0);
+      meanwhile();
       f32x16 s = {};
 #pragma unroll
       for (int i = 0; i < PRODUCTS; i++) {
@@ -417,12 +437,9 @@ __global__ __launch_bounds__(64 * RW) void tree_attention_kernel(TreeArgs a) {
       for (int i = 0; i < 16; i++) s[i] = bits >> (8 * (i >> 2) + (i & 3)) & 1 ? s[i] : -INFINITY;
     };
     // The reference follows the maximum only where a weight would pass 2^(8 + HEADROOM): in the first tiles, hardly ever later.
-    // fp16 weights start at 2^HEADROOM, so that small ones keep their bits.
-    auto settle = [&](const f32x16& s) {
+    // fp16 weights start at 2^HEADROOM, so that small ones keep their bits.  top: of this lane's scores
+    auto settle = [&](float top) {
       constexpr float HEADROOM = Mat<T>::EXPONENT == 0x7c00 ? 7.f : 0.f;
-      float top = s[0];
-#pragma unroll
-      for (int i = 1; i < 16; i++) top = fmaxf(top, s[i]);
       top = max_xor32(top) * a.scale;
       if (__ballot(top > st.m + (8.f + HEADROOM)) != 0) {
         const float m = fmaxf(st.m, top - HEADROOM), keep = st.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st.m - m);
@@ -430,6 +447,12 @@ __global__ __launch_bounds__(64 * RW) void tree_attention_kernel(TreeArgs a) {
         st.l *= keep;
         scale_sums<D / 32>(st.o, keep);
       }
+    };
+    auto top_of = [&](const f32x16& s) {
+      float top = s[0];
+#pragma unroll
+      for (int i = 1; i < 16; i++) top = fmaxf(top, s[i]);
+      return top;
     };
     s16x8 pf[2];
     auto weigh = [&](const f32x16& s, int i) {   // registers i and i + 1
@@ -441,9 +464,12 @@ __global__ __launch_bounds__(64 * RW) void tree_attention_kernel(TreeArgs a) {
       pf[i >> 3][i & 7] = __builtin_bit_cast(short, (T)w[0]);
       pf[i >> 3][(i & 7) + 1] = __builtin_bit_cast(short, (T)w[1]);
     };
-    auto sum_values = [&]() {
+    auto sum_values = [&](auto beside) {
 #pragma unroll
-      for (int i = 0; i < PRODUCTS; i++) st.o[i >> 1] = Mat<T>::mfma(vf[i], pf[i & 1], st.o[i >> 1]);
+      for (int i = 0; i < PRODUCTS; i++) {
+        st.o[i >> 1] = Mat<T>::mfma(vf[i], pf[i & 1], st.o[i >> 1]);
+        beside(i);
+      }
     };
     auto request_next = [&](int granule, int stage) {   // into the place of the stage in front of `stage`
       none = none << 2 | (next1 < 0) << 1 | (next0 < 0);
@@ -461,24 +487,26 @@ __global__ __launch_bounds__(64 * RW) void tree_attention_kernel(TreeArgs a) {
     if constexpr (AHEAD) {
       // scores one granule ahead: their products run beside the exponentials of the granule whose values are summed next
       arrived(g0, std::integral_constant<int, STAGES - 2>());
-      f32x16 s = scores(0, [](int) {});
+      f32x16 s = scores(0, [] {}, [](int) {});
       hide(s, g0, none >> (2 * (STAGES - 2)) & 3);
-      settle(s);
+      settle(top_of(s));
       for (int granule = g0; granule < g1; granule++) {
         arrived(granule + 1, std::integral_constant<int, STAGES - 3>());
-        request_next(granule, stage);
-        clean_values(granule, stage, none >> (2 * (STAGES - 1)) & 3);
+        clean_values(granule, stage, none >> (2 * (STAGES - 2)) & 3);
         const int stage1 = stage + 1 == STAGES ? 0 : stage + 1;
-        f32x16 s_next = scores(stage1, [&](int i) {
+        f32x16 s_next = scores(stage1, [&] { request_next(granule, stage); }, [&](int i) {
           read_values(stage, i);
 #pragma unroll
           for (int j = i * 8 / PRODUCTS; j < (i + 1) * 8 / PRODUCTS; j++) weigh(s, 2 * j);
         });
-        sum_values();
-        if (granule + 1 < g1) {
-          hide(s_next, granule + 1, none >> (2 * (STAGES - 2)) & 3);
-          settle(s_next);
-        }
+        if (granule + 1 < g1) hide(s_next, granule + 1, none >> (2 * (STAGES - 2)) & 3);
+        float top = s_next[0];
+        sum_values([&](int i) {
+#pragma unroll
+          for (int j = i * 16 / PRODUCTS; j < (i + 1) * 16 / PRODUCTS; j++) top = fmaxf(top, s_next[j]);
+          __builtin_amdgcn_sched_barrier(0);
+        });
+        if (granule + 1 < g1) settle(top);
         next_pages(granule);   // (reads that other reads would have to wait for, so: when there are none)
         s = s_next;
         stage = stage1;
@@ -486,14 +514,13 @@ __global__ __launch_bounds__(64 * RW) void tree_attention_kernel(TreeArgs a) {
     } else {
       for (int granule = g0; granule < g1; granule++) {
         arrived(granule, std::integral_constant<int, STAGES - 2>());
-        request_next(granule, stage);
-        clean_values(granule, stage, none >> (2 * (STAGES - 1)) & 3);
-        f32x16 s = scores(stage, [&](int i) { read_values(stage, i); });
+        clean_values(granule, stage, none >> (2 * (STAGES - 2)) & 3);
+        f32x16 s = scores(stage, [&] { request_next(granule, stage); }, [&](int i) { read_values(stage, i); });
         hide(s, granule, none >> (2 * (STAGES - 1)) & 3);
-        settle(s);
+        settle(top_of(s));
 #pragma unroll
         for (int i = 0; i < 16; i += 2) weigh(s, i);
-        sum_values();
+        sum_values([](int) {});
         next_pages(granule);
         stage = stage + 1 == STAGES ? 0 : stage + 1;
       }
@@ -534,7 +561,7 @@ __global__ __launch_bounds__(64 * RW) void tree_attention_kernel(TreeArgs a) {
         }
       }
     } else {
-      const size_t slot = ((size_t)blockIdx.x * 2 + (g0 == 0)) * ROWS + rw * 32 + (lane & 31);
+      const size_t slot = ((size_t)mine_run * 2 + (g0 == 0)) * ROWS + rw * 32 + (lane & 31);
       float* out = a.part_o + slot * D;
 #pragma unroll
       for (int b = 0; b < D / 32; b++) {
@@ -551,7 +578,7 @@ __global__ __launch_bounds__(64 * RW) void tree_attention_kernel(TreeArgs a) {
   }
 }
 
-// The rows of units that several blocks had a part in: sum_z 2^(m_z - m) o_z / sum_z 2^(m_z - m) l_z, in the order of the blocks.  WPR
+// The rows of units that several blocks had a part in: sum_z 2^(m_z - m) o_z / sum_z 2^(m_z - m) l_z, in the order of the keys.  WPR
 // waves share out a row's parts, D / 64 numbers per lane: 8 where units are so few that each has many, one where they are many.
 template <class T, int D, int RW, int WPR>
 __global__ __launch_bounds__(512) void tree_merge_kernel(TreeArgs a) {
@@ -566,19 +593,25 @@ __global__ __launch_bounds__(512) void tree_merge_kernel(TreeArgs a) {
   const int total = min(length_of(p, seq) + rows.y, p.max_pages * p.page_tokens);
   const int granules = div_up(total, GRANULE), row_tiles = div_up(rows.y * a.group, ROWS), row_tile = r / ROWS;
   const Cut cut = *a.cut;
-  const int first = (seq > 0 ? a.upto[seq - 1] : 0) + (kv_head * row_tiles + row_tile) * cut.length(granules) + cut.front();
-  const int b0 = first / cut.run, b1 = (first + granules - 1) / cut.run;
-  if (b0 == b1) return;
-  auto slot_of = [&](int block) { return ((size_t)block * 2 + (first >= block * cut.run)) * ROWS + r % ROWS; };
+  const int before = (seq > 0 ? a.upto[seq - 1] : 0) + kv_head * row_tiles * cut.length(granules);
+  int run0, parts, step = 1;   // the runs that had a part
+  if (cut.whole) {
+    run0 = before / cut.run + row_tile, parts = cut.parts(granules), step = row_tiles;
+  } else {
+    const int first = before + row_tile * (granules + START) + START;
+    run0 = first / cut.run, parts = (first + granules - 1) / cut.run - run0 + 1;
+  }
+  if (parts < 2) return;
+  auto slot_of = [&](int part) { return ((size_t)(run0 + part * step) * 2 + (part == 0)) * ROWS + r % ROWS; };
   float m = -INFINITY;
-  for (int b = b0 + lane; b <= b1; b += 64) m = fmaxf(m, a.part_ml[slot_of(b)].x);
+  for (int i = lane; i < parts; i += 64) m = fmaxf(m, a.part_ml[slot_of(i)].x);
   for (int i = 32; i > 0; i >>= 1) m = fmaxf(m, __shfl_xor(m, i));
   const float safe = m == -INFINITY ? 0.f : m;
   Vec o = {};
   float l = 0.f;
 #pragma unroll 4
-  for (int b = b0 + share; b <= b1; b += WPR) {
-    const size_t slot = slot_of(b);
+  for (int i = share; i < parts; i += WPR) {
+    const size_t slot = slot_of(i);
     const float2 ml = a.part_ml[slot];
     const float c = __builtin_amdgcn_exp2f(ml.x - safe);
     o += c * *reinterpret_cast<const Vec*>(a.part_o + slot * D + lane * PER);
