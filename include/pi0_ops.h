@@ -162,7 +162,7 @@ int pi0_qk_norm_rope(const pi0_pages* pages, int layer, const pi0_rows* q, const
  *     out = sum_j softmax_j(scale * q . k_j) v_j        over what the token sees; 0 if that is nothing
  * What a token does not see does not reach it, whatever is stored there (a NaN, an unwritten page).
  *   q, out    n_rows rows of `heads` heads, a multiple of kv_heads; both of the cache's type; out may be q itself
- *   max_rows  most new tokens of a sequence, 1 .. 1024; n_seqs * kv_heads * ceil(max_rows * heads / kv_heads / 32) *
+ *   max_rows  most new tokens of a sequence, 1 .. 1024; n_seqs * kv_heads * ceil(max_rows * heads / kv_heads / 16) *
  *             (max_pages * page_tokens / 32 + 7) below 2^30
  *   d_mask    uint32 [n_rows][mask_words], or NULL (mask_words 0); bits behind the last word are clear
  * Products on matrix cores with fp32 sums, softmax in fp32, its weights rounded to the cache's type in front of the second

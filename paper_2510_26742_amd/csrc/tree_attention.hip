@@ -1,14 +1,19 @@
 // Attention of drafted tokens over a paged key/value cache (pi0_tree_attention).
 //
 // All query heads of a key/value head, times all new tokens of a sequence, are rows of one product: K and V are read once
-// for all of them.  One pass over the keys in tiles of 32 with a running maximum and sum:
-//     S^T = K Q^T  (32 keys x 32 rows, mfma 32x32x16),  p = exp2(scale log2(e) S - m),  O^T += V^T P^T
-// S^T leaves a lane one row and 16 of its 32 keys, which is how the second product takes its right operand if the keys
-// of a step of 16 are counted as they lie there: probabilities go from one product into the next without leaving their
-// lane, row sums and maxima need one exchange between the two halves of a wave.  V^T is read out of row-major tiles with
-// the transposing LDS load (4 keys x 16 d per 16 lanes).
+// for all of them.  One pass over the keys, 32 at a time, with a running maximum and sum:
+//     S^T = K Q^T  (16 keys x 16 rows, mfma 16x16x32),  p = exp2(scale log2(e) S - m),  O^T += V^T P^T
+// S^T leaves a lane one row and 4 of 16 keys, which is how the second product takes its right operand if the keys of its 32
+// are counted as they lie there: probabilities go from one product into the next without leaving their lane, row sums and
+// maxima need two exchanges between the quarters of a wave.  V^T is read out of row-major tiles with the transposing LDS
+// load (4 keys x 16 d per 16 lanes).  A wave has R times 16 rows: what it reads of K and V out of LDS serves all of them.  R = 1 where
+// the cache's own bytes are what the time goes to (up to 64 rows), 2 where there are more.
+// What bounds it: few rows the reads of the cache (64 x 1 token, 8 heads over 1 of 256, up to 8192 keys: 277 MB in 50 us, 5.5 TB/s);
+// many rows the issue of instructions, of which a wave that is alone on its SIMD has one per 4 cycles (8 x 64 nodes over 16384: 470
+// TFLOP/s; a granule's 64 products per wave could end in 1024 cycles and take 1900), which is why the loop does nothing that
+// can be done in front of it.
 // Tiles come straight into LDS, 16 bytes per lane; the pieces of a row are permuted by its key (on the global side: a lane
-// may fetch any piece) so that neither product's reads collide in the banks. 
+// may fetch any piece) so that neither product's reads collide in the banks.
 #include "pages_common.h"
 #include "exec_ctx.h"
 
@@ -20,54 +25,54 @@ typedef f16 f16x2 __attribute__((ext_vector_type(2)));
 typedef f16 f16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x8 __attribute__((ext_vector_type(8)));
 
 template <class T>
 struct Mat;
 template <>
 struct Mat<bf16> {
   static constexpr unsigned EXPONENT = 0x7f80;
-  static __device__ __forceinline__ f32x16 mfma(s16x8 a, s16x8 b, f32x16 c) {
-    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  static __device__ __forceinline__ f32x4 mfma(s16x8 a, s16x8 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
   }
 };
 template <>
 struct Mat<f16> {
   static constexpr unsigned EXPONENT = 0x7c00;
-  static __device__ __forceinline__ f32x16 mfma(s16x8 a, s16x8 b, f32x16 c) {
-    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  static __device__ __forceinline__ f32x4 mfma(s16x8 a, s16x8 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
   }
 };
 
-
-// How the work is cut.  A unit is a tile of 32 RW rows of one sequence and key/value head against all of its keys, in granules of 32
+// How the work is cut.  A unit is a tile of 16 R RW rows of one sequence and key/value head against all of its keys, in granules of 32
 // keys.  Lengths differ, and the host does not know them, so every block works out from the lengths which granules are its
 // own: the units lie behind each other on a line that is cut into runs of equal length, one per block.
 //   - Few units (at most half as many as blocks): each takes up a whole number of runs, so that a block has part of one unit
 //     only; the shortest run, in steps of an eighth, for which there are blocks enough.  The row tiles of a head lie side by side, part
-//     by part, and neighbouring runs go to blocks of one die: its L2 gives the same keys to all of them (8 x 64 nodes over
-//     16384, four tiles of 128 rows: TODO us, with the tiles behind each other 45).
+//     by part, and neighbouring runs go to blocks of one die: its L2 gives the same keys to all of them.
 //   - Many: the line is dense, except that a unit is START granules longer than it is - what a block spends before a unit's
 //     first granule and behind its last -, and a run may end one unit, hold others and begin the next.
 // A block writes a unit that it has all of; of any other it leaves a partial result, in slot 1 if it has the first granule, in slot 0
 // if not, and the second launch joins them.
 constexpr int GRANULE = 32, START = 6;
 
-// A stage of K and V tiles is 128 D bytes; STAGES of them per block.  With one row tile per wave and 256 d the registers hold one
-// wave per SIMD.  Few rows: what counts is bytes in flight and, beside them, other blocks that read while one begins or
-// ends a unit, so blocks are small and several share a compute unit.  BLOCKS: as many as the chip's 256 hold at once.
-template <int D, int RW>
+// A stage of K and V tiles is 128 D bytes; STAGES of them per block.  Few rows: what counts is bytes in flight and, beside them,
+// other blocks that read while one begins or ends a unit, so blocks are small and several share a compute unit.  BLOCKS: as
+// many as the chip's 256 hold at once.
+template <int D, int RW, int R>
 struct Shape;
-template <> struct Shape<256, 1> { static constexpr int STAGES = 2, BLOCKS = 512; };
-template <> struct Shape<256, 2> { static constexpr int STAGES = 2, BLOCKS = 512; };
-template <> struct Shape<256, 4> { static constexpr int STAGES = 4, BLOCKS = 256; };
-template <> struct Shape<128, 1> { static constexpr int STAGES = 2, BLOCKS = 1024; };
-template <> struct Shape<128, 2> { static constexpr int STAGES = 4, BLOCKS = 512; };
-template <> struct Shape<128, 4> { static constexpr int STAGES = 4, BLOCKS = 512; };
-template <> struct Shape<128, 8> { static constexpr int STAGES = 4, BLOCKS = 256; };
-template <> struct Shape<64, 1> { static constexpr int STAGES = 4, BLOCKS = 1024; };
-template <> struct Shape<64, 2> { static constexpr int STAGES = 4, BLOCKS = 1024; };
-template <> struct Shape<64, 4> { static constexpr int STAGES = 4, BLOCKS = 512; };
-template <> struct Shape<64, 8> { static constexpr int STAGES = 4, BLOCKS = 512; };
+template <> struct Shape<256, 1, 1> { static constexpr int STAGES = 2, BLOCKS = 512; };
+template <> struct Shape<256, 2, 1> { static constexpr int STAGES = 2, BLOCKS = 512; };
+template <> struct Shape<256, 4, 1> { static constexpr int STAGES = 2, BLOCKS = 512; };
+template <> struct Shape<256, 4, 2> { static constexpr int STAGES = 4, BLOCKS = 256; };
+template <> struct Shape<128, 1, 1> { static constexpr int STAGES = 2, BLOCKS = 1024; };
+template <> struct Shape<128, 2, 1> { static constexpr int STAGES = 4, BLOCKS = 512; };
+template <> struct Shape<128, 4, 1> { static constexpr int STAGES = 4, BLOCKS = 512; };
+template <> struct Shape<128, 4, 2> { static constexpr int STAGES = 4, BLOCKS = 512; };
+template <> struct Shape<64, 1, 1> { static constexpr int STAGES = 4, BLOCKS = 1024; };
+template <> struct Shape<64, 2, 1> { static constexpr int STAGES = 4, BLOCKS = 1024; };
+template <> struct Shape<64, 4, 1> { static constexpr int STAGES = 4, BLOCKS = 512; };
+template <> struct Shape<64, 4, 2> { static constexpr int STAGES = 4, BLOCKS = 512; };
 
 // Where a unit lies on the line.  length: of the unit's share of the line, front: how far behind its beginning the first granule is
 struct Cut {
@@ -98,11 +103,10 @@ struct TreeArgs {
   float2* part_ml;       // [runs][2][rows of a tile]: reference of the exponents, sum of the weights
 };
 
-// page_at for a sequence and entry that are the same for the whole wave: through the scalar cache, so that it does not
-// wait in line behind the tiles that are on their way
-__device__ __forceinline__ int uniform_page(const pi0_pages& p, int seq, int idx) {
-  const int page = ((const __attribute__((address_space(4))) int*)p.d_table)[(size_t)seq * p.max_pages + min(idx, p.max_pages - 1)];
-  return idx < p.max_pages && page >= 0 && page < p.n_pages ? page : -1;
+// A sequence's entry idx, the same for the whole wave: through the scalar cache, so that it does not wait in line behind the tiles
+// that are on their way
+__device__ __forceinline__ int entry_at(const pi0_pages& p, int seq, int idx) {
+  return ((const __attribute__((address_space(4))) int*)p.d_table)[(size_t)seq * p.max_pages + min(idx, p.max_pages - 1)];
 }
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
@@ -111,27 +115,28 @@ __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirs
 typedef const __attribute__((address_space(3))) s16x8* LdsPiece;
 typedef __attribute__((address_space(3))) s16x4* LdsQuad;
 
-// S^T has a lane own one row of queries: lane = column (row of queries) + 32 h, register i = key 8 (i / 4) + 4 h + i % 4; O^T the
-// same with d in the place of keys.
+// S^T has a lane own one row of queries: lane = column (row of queries) + 16 quad, register i = key 4 quad + i; O^T the same with d in
+// the place of keys.
 template <int D>
 struct RowState {
-  f32x16 o[D / 32];
-  float m, l;   // reference of the exponents, sum of this lane's weights
+  f32x4 o[D / 16];
+  float m, l;    // reference of the exponents, sum of this lane's weights
+  float shift;   // -m, 0 where that is infinite
 };
 
 __device__ __forceinline__ float dot_ones(bf16x2 w, float c) { return __builtin_amdgcn_fdot2_f32_bf16(w, bf16x2{(bf16)1.0f, (bf16)1.0f}, c, false); }
 __device__ __forceinline__ float dot_ones(f16x2 w, float c) { return __builtin_amdgcn_fdot2(w, f16x2{(f16)1.0f, (f16)1.0f}, c, false); }
 
 // o *= c, where it is: in the accumulation registers.  Written as a product, the sums are copied to vector registers in every round, whether
-// or not the branch is taken (128 instructions at D = 256).  The products that wrote them have long ended - the scores
+// or not the branch is taken (64 instructions at D = 256).  The products that wrote them have long ended - the scores
 // that decided the branch are a later product's - and the waits in front and behind cover the longest there is.
 template <int N>
-__device__ __forceinline__ void scale_sums(f32x16 (&o)[N], float c) {
+__device__ __forceinline__ void scale_sums(f32x4 (&o)[N], float c) {
   asm volatile("s_nop 15\n\ts_nop 15\n\ts_nop 15\n\ts_nop 15" ::: "memory");
 #pragma unroll
   for (int b = 0; b < N; b++) {
 #pragma unroll
-    for (int i = 0; i < 16; i++) {
+    for (int i = 0; i < 4; i++) {
       float x = o[b][i], t;
       asm volatile("v_accvgpr_read_b32 %1, %0\n\tv_mul_f32 %1, %1, %2\n\tv_accvgpr_write_b32 %0, %1" : "+a"(x), "=&v"(t) : "v"(c));
       o[b][i] = x;
@@ -182,20 +187,20 @@ __device__ __forceinline__ int wave_prefix(int v) {   // sum over the lanes up t
   return v;
 }
 
-// RW waves of a block have 32 rows each and read the same tiles
-template <class T, int D, int RW>
-__global__ __launch_bounds__(64 * RW) void tree_attention_kernel(TreeArgs a) {
-  constexpr int STAGES = Shape<D, RW>::STAGES, BLOCKS = Shape<D, RW>::BLOCKS, ROWS = 32 * RW;
+// RW waves of a block have R times 16 rows each and read the same tiles
+template <class T, int D, int RW, int R>
+__global__ __launch_bounds__(64 * RW, RW >= 4 && (D < 256 || R == 1) ? 2 : 1) void tree_attention_kernel(TreeArgs a) {
+  constexpr int STAGES = Shape<D, RW, R>::STAGES, BLOCKS = Shape<D, RW, R>::BLOCKS, ROWS = 16 * R * RW;
   constexpr int PIECES = D / 8, TILE = 32 * D * 2, PARTS = TILE / 1024, REQUESTS = 2 * PARTS / RW, KEYS_PER_REQUEST = 512 / D;
-  constexpr bool AHEAD = RW >= 4;
-  constexpr int PRODUCTS = D / 16;   // of either kind, per granule
-  static_assert(REQUESTS >= 1 && STAGES >= (AHEAD ? 3 : 2) && (STAGES - 2) * REQUESTS < 64, "the wait counter holds what is in flight");
+  constexpr bool AHEAD = R > 1;
+  constexpr int STEPS = D / 32, TILES = D / 16;   // of 32 d that scores are summed over, of 16 d that sums are kept for
+  static_assert(REQUESTS >= 1 && STAGES >= (AHEAD ? 3 : 2) && (!AHEAD || RW == 4) && (STAGES - 2) * REQUESTS < 64, "the wait counter holds what is in flight");
   typedef T T2 __attribute__((ext_vector_type(2)));
   typedef T T4 __attribute__((ext_vector_type(4)));
   const pi0_pages& p = a.p;
   __shared__ __align__(1024) unsigned char tiles[STAGES][2][TILE];
   __shared__ int2 line_of[MAX_SEQS];   // units and granules of a sequence, then where its share of the line ends (x)
-  const int lane = threadIdx.x & 63, rw = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
+  const int lane = threadIdx.x & 63, rw = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), quad = lane >> 4;
 
   // The line, worked out by every wave for itself: lane l has the sequences l, l + 64, ..; what it knows of the first 64 stays in
   // registers.  (Whatever runs once per block is written to be short: a block starts with its code far away, and 64 bytes
@@ -255,14 +260,14 @@ __global__ __launch_bounds__(64 * RW) void tree_attention_kernel(TreeArgs a) {
   const int mine_run = (blockIdx.x & 7) * (BLOCKS / 8) + (blockIdx.x >> 3);
   const int begin = (int)min((int64_t)line, (int64_t)mine_run * cut.run), end = (int)min((int64_t)line, (int64_t)begin + cut.run);
 
-  // This lane's pieces.  First product: key lane % 32, pieces h, h + 2, ..; second: of 4 keys and 16 d that 16 lanes read transposed,
-  // key (lane % 16) / 4 and quad lane % 4.  Requests: row lane / PIECES of a KiB, its piece lane % PIECES - where the row's
-  // permuted piece lies in the cache.
-  const int kkey = lane & 31, vkey = (lane & 15) >> 2;
-  const unsigned read_k = kkey * 2 * D + (((D == 64 ? (kkey >> 1) & 7 : kkey & 15) ^ h) << 4);
-  const unsigned read_v = (4 * h + vkey) * 2 * D + ((D == 64 ? (vkey >> 1) & 1 : vkey) << 6) + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
+  // This lane's pieces.  First product: keys lane % 16 and that + 16, pieces quad, quad + 4, ..; second: of 4 keys and 16 d that 16
+  // lanes read transposed, key (lane % 16) / 4 and 4 d of lane % 4.  Requests: row lane / PIECES of a KiB, its piece lane % PIECES -
+  // where the row's permuted piece lies in the cache.
+  const int kkey = lane & 15, vkey = 4 * quad + (kkey >> 2);
+  const unsigned read_k = kkey * 2 * D + (((D == 64 ? kkey >> 1 : kkey) ^ quad) << 4);
+  const unsigned read_v = vkey * 2 * D + ((D == 64 ? (vkey >> 1) & 3 : vkey & 7) << 5) + (lane & 3) * 8;
   const int my_row = lane / PIECES, my_piece = lane % PIECES;
-  const int piece_k0 = my_piece ^ (D == 64 ? (my_row >> 1) & 7 : my_row), piece_v0 = my_piece ^ (D == 64 ? ((my_row >> 1) & 1) << 2 : (my_row & 3) << 2);
+  const int piece_k0 = my_piece ^ (D == 64 ? (my_row >> 1) & 7 : my_row), piece_v0 = my_piece ^ ((D == 64 ? (my_row >> 1) & 3 : my_row) << 1);
   const int shift = 31 - __clz(p.page_tokens), in_page = p.page_tokens - 1;
   const unsigned lds0 = lds_address(&tiles[0][0][0]);
 
@@ -305,68 +310,103 @@ __global__ __launch_bounds__(64 * RW) void tree_attention_kernel(TreeArgs a) {
       if (g0 >= g1) continue;   // the run ends in front of the unit's first granule
     }
 
-    // this lane's row: token and head
-    const int r = row_tile * ROWS + rw * 32 + (lane & 31);
-    const bool live = r < rows.y * a.group;
-    // r / group: both below 2^20, and half a row is more than the reciprocal is off by
-    const int node = live ? (int)(((float)r + 0.5f) * __builtin_amdgcn_rcpf((float)a.group)) : 0, head = kv_head * a.group + (live ? r - node * a.group : 0);
-    s16x8 q[D / 16];   // (a lane without a row takes the tile's first token's, and gives nothing back)
-    const T* const q_row = reinterpret_cast<const T*>(a.q) + (rows.x + node) * a.q_row_stride + head * a.q_head_stride + h * 8;
+    // this lane's rows: token and head
+    int node[R], head[R];
+    bool live[R];
+    const unsigned* mask[R];
+    s16x8 q[R][STEPS];   // (a lane without a row takes the first token's, and gives nothing back)
 #pragma unroll
-    for (int i = 0; i < D / 16; i++) q[i] = *reinterpret_cast<const s16x8*>(q_row + i * 16);
+    for (int n = 0; n < R; n++) {
+      const int r = row_tile * ROWS + (rw * R + n) * 16 + kkey;
+      live[n] = r < rows.y * a.group;
+      // r / group: both below 2^20, and half a row is more than the reciprocal is off by
+      node[n] = live[n] ? (int)(((float)r + 0.5f) * __builtin_amdgcn_rcpf((float)a.group)) : 0;
+      head[n] = kv_head * a.group + (live[n] ? r - node[n] * a.group : 0);
+      mask[n] = a.mask + (size_t)(rows.x + node[n]) * a.mask_words;
+      const T* const q_row = reinterpret_cast<const T*>(a.q) + (rows.x + node[n]) * a.q_row_stride + head[n] * a.q_head_stride + quad * 8;
+#pragma unroll
+      for (int i = 0; i < STEPS; i++) q[n][i] = *reinterpret_cast<const s16x8*>(q_row + i * 32);
+    }
     if (a.odd_scale) {
 #pragma unroll
-      for (int i = 0; i < D / 16; i++) q[i] = (q[i] ^ a.negate) & a.q_bits;
+      for (int n = 0; n < R; n++) {
+#pragma unroll
+        for (int i = 0; i < STEPS; i++) q[n][i] = (q[n][i] ^ a.negate) & a.q_bits;
+      }
     }
-    const unsigned* mask = a.mask != nullptr ? a.mask + (size_t)(rows.x + node) * a.mask_words : nullptr;
     const char* const pool_k = reinterpret_cast<const char*>(p.d_k) + 2 * (a.layer + kv_head * p.head_stride);
     const char* const pool_v = reinterpret_cast<const char*>(p.d_v) + 2 * (a.layer + kv_head * p.head_stride);
 
-    // Requests this wave's part of a granule, of whose keys the first and last 16 lie in pages page0 and page1.  Where there is no page
+    // Requests of this wave's part of a granule, of whose keys the first and last 16 lie in pages page0 and page1.  Where there is no page
     // (-1), and behind the last position, some row is read that the scores then hide.  A quarter of a granule is 16 keys, or the
-    // values of 16; a wave has several quarters, one, or half of one.
-    constexpr int QUARTER = PARTS / 2, SHARE = RW > 4 ? QUARTER / (RW / 4) : QUARTER;   // KiB
+    // values of 16; a wave has one, two or all four.
+    constexpr int QUARTER = PARTS / 2;   // KiB
+    struct Quarter {
+      const char* from;
+      unsigned to;
+    };
+    auto quarter_of = [&](int quarter, int granule, int stage, int page0, int page1) {
+      const int pos = granule * GRANULE + (quarter & 1) * 16, page = max(quarter & 1 ? page1 : page0, 0);
+      const uint64_t in = (uint64_t)(unsigned)(pos & in_page) * (unsigned)p.token_stride;
+      return Quarter{(quarter >= 2 ? pool_v : pool_k) + 2 * (page * p.page_stride + in), lds0 + stage * 2 * TILE + quarter * QUARTER * 1024};
+    };
+    auto request_kib = [&](const Quarter& at, bool of_v, int kib) {
+      // how far the first key's number turns the pieces of its row (the rest is in piece0)
+      const int key = kib * KEYS_PER_REQUEST, turn_k = D == 64 ? key >> 1 & 7 : key, turn_v = D == 64 ? 0 : (key & 7) << 1;
+      // (15 strides and a row fit 32 bits)
+      const unsigned off = (my_row + key) * (unsigned)(2 * p.token_stride) + ((of_v ? piece_v0 : piece_k0) ^ (of_v ? turn_v : turn_k)) * 16;
+      asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(at.to), "v"(off), "s"(at.from), "n"(kib * 1024) : "memory", "scc");
+    };
     auto request = [&](int granule, int stage, int page0, int page1) {
-      const int pos0 = granule * GRANULE;
-      const unsigned off = my_row * (unsigned)(2 * p.token_stride), to = lds0 + stage * 2 * TILE;
-      const int64_t at0 = 2 * (max(page0, 0) * p.page_stride + (pos0 & in_page) * p.token_stride);
-      const int64_t at1 = 2 * (max(page1, 0) * p.page_stride + ((pos0 + 16) & in_page) * p.token_stride);
 #pragma unroll 1
-      for (int quarter = RW > 4 ? rw / (RW / 4) : rw; quarter < 4; quarter += RW) {
-        const bool of_v = quarter >= 2;
-        const int kib0 = RW > 4 ? rw % (RW / 4) * SHARE : 0;
-        const char* const from = (of_v ? pool_v : pool_k) + (quarter & 1 ? at1 : at0);
-        const int piece0 = of_v ? piece_v0 : piece_k0;
+      for (int quarter = rw; quarter < 4; quarter += RW) {
+        const Quarter at = quarter_of(quarter, granule, stage, page0, page1);
 #pragma unroll
-        for (int j = 0; j < SHARE; j++) {
-          const int kib = kib0 + j, key = kib * KEYS_PER_REQUEST;   // of the quarter, and its first key
-          // key's bits that turn the pieces; of a value's, only those that are not the same for the whole quarter
-          const int turn_k = D == 64 ? ((quarter & 1) * 16 + key) >> 1 & 7 : key, turn_v = D == 64 ? (key >> 1 & 1) << 2 : (key & 3) << 2;
-          request_to_lds(from + key * (2 * p.token_stride), off + (piece0 ^ (of_v ? turn_v : turn_k)) * 16, to + (quarter * QUARTER + kib) * 1024);
-        }
+        for (int kib = 0; kib < QUARTER; kib++) request_kib(at, quarter >= 2, kib);
       }
     };
-    auto page_of = [&](int granule, int half) {
-      return uniform_page(p, seq, (granule * GRANULE + half * 16) >> shift);
-    };
 
-    RowState<D> st;
+    RowState<D> st[R];
 #pragma unroll
-    for (int b = 0; b < D / 32; b++) st.o[b] = f32x16{};
-    st.m = -INFINITY;
-    st.l = 0.f;
+    for (int n = 0; n < R; n++) {
+#pragma unroll
+      for (int b = 0; b < TILES; b++) {
+        st[n].o[b] = f32x4{};
+        asm volatile("" : "+a"(st[n].o[b]));   // (where they stay; the compiler would move them back and forth)
+      }
+      st[n].m = -INFINITY;
+      st[n].shift = 0.f;
+      st[n].l = 0.f;
+    }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // from here on only the tiles' requests are in flight
     __syncthreads();                                   // what was in the tiles has been read
     unsigned none = 0;   // two bits per granule, the latest requested lowest: its first, last 16 keys are on no page
-    int pages[STAGES][2];
+    int entry0, entry1, page0, page1;
+    auto next_entries = [&](int granule) {
+      entry0 = entry_at(p, seq, granule * GRANULE >> shift), entry1 = entry_at(p, seq, (granule * GRANULE + 16) >> shift);
+    };
+    auto next_pages = [&] {
+      page0 = (unsigned)entry0 < (unsigned)p.n_pages ? entry0 : -1, page1 = (unsigned)entry1 < (unsigned)p.n_pages ? entry1 : -1;
+      none = none << 2 | (page1 < 0) << 1 | (page0 < 0);
+    };
+    // With AHEAD the last granule is requested again where there is none behind it, into a stage that nobody reads any more: as
+    // many requests are on their way at the end as anywhere, and no branch parts the products.
+    auto in_unit = [&](int granule) { return AHEAD ? min(granule, g1 - 1) : granule; };
+    {
+      int entries[STAGES - 1][2];
 #pragma unroll
-    for (int i = 0; i < STAGES; i++) pages[i][0] = page_of(g0 + i, 0), pages[i][1] = page_of(g0 + i, 1);
+      for (int i = 0; i < STAGES - 1; i++) {
+        next_entries(in_unit(g0 + i));
+        entries[i][0] = entry0, entries[i][1] = entry1;
+      }
 #pragma unroll
-    for (int i = 0; i < STAGES - 1; i++) {
-      none = none << 2 | (pages[i][1] < 0) << 1 | (pages[i][0] < 0);
-      if (g0 + i < g1) request(g0 + i, i, pages[i][0], pages[i][1]);
+      for (int i = 0; i < STAGES - 1; i++) {
+        entry0 = entries[i][0], entry1 = entries[i][1];
+        next_pages();
+        if (AHEAD || g0 + i < g1) request(in_unit(g0 + i), i, page0, page1);
+      }
     }
-    int next0 = pages[STAGES - 1][0], next1 = pages[STAGES - 1][1];
+    next_entries(in_unit(g0 + STAGES - 1));
 
     int odd_from = g1;   // first granule with such values
     // A weight of zero does not silence an infinity or a NaN.  Committed values are seen by every row; where there is anything
@@ -382,207 +422,243 @@ __global__ __launch_bounds__(64 * RW) void tree_attention_kernel(TreeArgs a) {
         __syncthreads();
       }
     };
-    // The scores of a granule.  All of its keys' pieces are asked for first: left to itself the compiler puts a read right in front of
-    // the product that takes it, which then waits for the whole way to shared memory and back.  meanwhile() is done on that way,
-    // beside(i) goes with product i.
-    auto scores = [&](int stage, auto meanwhile, auto beside) {
+    // The scores of a granule.  Reads of shared memory run LEAD steps in front of the products that take them (left to itself the
+    // compiler puts a read right in front of its product, which then waits for the whole way there and back).  beside(i) goes
+    // with the products of step i.  Of a result, 4 are of keys 4 quad .., 4 of those 16 further on.
+    constexpr int LEAD = 3, LEAD_V = 4;
+    auto scores = [&](int stage, f32x8 (&s)[R], auto beside) {
       const unsigned at = lds0 + stage * 2 * TILE;
-      s16x8 kf[PRODUCTS];
+      s16x8 kf[STEPS][2];
+      f32x4 sum[R][2];
+      auto read_keys = [&](int i) {
 #pragma unroll
-      for (int i = 0; i < PRODUCTS; i++) kf[i] = *((LdsPiece)(size_t)(at + (read_k ^ ((2 * i & 14) << 4))) + (2 * i & 16));
+        for (int t = 0; t < 2; t++) kf[i][t] = *((LdsPiece)(size_t)(at + (read_k ^ ((4 * i & 12) << 4)) + t * 32 * D) + (4 * i & 16));
+      };
+#pragma unroll
+      for (int i = 0; i < (LEAD < STEPS ? LEAD : STEPS); i++) read_keys(i);
       __builtin_amdgcn_sched_barrier(0);
-      meanwhile();
-      f32x16 s = {};
 #pragma unroll
-      for (int i = 0; i < PRODUCTS; i++) {
-        s = Mat<T>::mfma(kf[i], q[i], s);
+      for (int i = 0; i < STEPS; i++) {
+        if (i + LEAD < STEPS) read_keys(i + LEAD);
+#pragma unroll
+        for (int n = 0; n < R; n++) {
+#pragma unroll
+          for (int t = 0; t < 2; t++) sum[n][t] = Mat<T>::mfma(kf[i][t], q[n][i], i == 0 ? f32x4{} : sum[n][t]);
+        }
         beside(i);
         __builtin_amdgcn_sched_barrier(0);
       }
-      return s;
+#pragma unroll
+      for (int n = 0; n < R; n++) s[n] = __builtin_shufflevector(sum[n][0], sum[n][1], 0, 1, 2, 3, 4, 5, 6, 7);
     };
-    s16x8 vf[PRODUCTS];
-    auto read_values = [&](int stage, int i) {   // for product i
-      const int b = i >> 1, step = i & 1;
-      const unsigned at = lds0 + stage * 2 * TILE + TILE + (read_v ^ ((b & 3) << 6)) + (b >> 2) * 256 + step * 16 * 2 * D;
+    s16x8 vf[TILES];
+    auto read_values = [&](int stage, int i) {   // of tile i
+      const unsigned at = lds0 + stage * 2 * TILE + TILE + (read_v ^ ((i & 7) << 5)) + (i >> 3) * 256;
       const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsQuad)(size_t)at);
-      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsQuad)(size_t)(at + 8 * 2 * D));
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsQuad)(size_t)(at + 32 * D));
       vf[i] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
     };
-    // what of a tile the row does not see becomes minus infinity.  gone: its first, last 16 keys are on no page
-    auto hide = [&](f32x16& s, int granule, unsigned gone) {
+    auto first_values = [&](int stage, int step) {   // those of the first LEAD_V tiles, with the last two steps of the scores
+#pragma unroll
+      for (int i = 0; i < LEAD_V / 2; i++) {
+        if (step >= STEPS - 2) read_values(stage, (step - (STEPS - 2)) * (LEAD_V / 2) + i);
+      }
+    };
+    // what of a tile the rows do not see becomes minus infinity.  gone: its first, last 16 keys are on no page
+    auto hide = [&](f32x8 (&s)[R], int granule, unsigned gone) {
       const int pos0 = granule * GRANULE, j0 = pos0 - length;   // node at the tile's first key
       if (j0 + GRANULE <= 0 && gone == 0) return;
-      unsigned seen = 0xffffffffu;      // a bit per key
-      if (j0 + GRANULE > 0) {
-        unsigned nodes = 0;             // bit b: node max(j0, 0) + b
-        const int jn = max(j0, 0);
-        if (mask != nullptr) {
+      unsigned on_page = 0xffffffffu;
+      if (gone & 1) on_page &= 0xffff0000u;
+      if (gone & 2) on_page &= 0x0000ffffu;
+      const int have = total - pos0, committed = min(32, max(0, -j0)), jn = max(j0, 0);
+      if (have < 32) on_page &= have > 0 ? (1u << have) - 1 : 0u;
+#pragma unroll
+      for (int n = 0; n < R; n++) {
+        unsigned nodes = 0;             // bit b: node jn + b
+        if (a.mask != nullptr) {
           const int word = jn >> 5, off = jn & 31;
-          const unsigned lo = word < a.mask_words ? mask[word] : 0, hi = word + 1 < a.mask_words ? mask[word + 1] : 0;
+          const unsigned lo = word < a.mask_words ? mask[n][word] : 0, hi = word + 1 < a.mask_words ? mask[n][word + 1] : 0;
           nodes = (unsigned)(((unsigned long long)hi << 32 | lo) >> off);
         } else {
-          const int visible = node - jn + 1;
+          const int visible = node[n] - jn + 1;
           nodes = visible >= 32 ? 0xffffffffu : visible > 0 ? (1u << visible) - 1 : 0u;
         }
-        const int committed = min(32, max(0, -j0));
-        seen = committed >= 32 ? 0xffffffffu : (1u << committed) - 1 | nodes << committed;
-        const int have = total - pos0;
-        if (have < 32) seen &= have > 0 ? (1u << have) - 1 : 0u;
-      }
-      if (gone & 1) seen &= 0xffff0000u;
-      if (gone & 2) seen &= 0x0000ffffu;
-      const unsigned bits = seen >> (4 * h);   // bit 8 (i / 4) + i % 4 is register i's key
+        // a bit per key
+        const unsigned seen = on_page & (committed >= 32 ? 0xffffffffu : (1u << committed) - 1 | nodes << committed);
+        const unsigned bits = seen >> (4 * quad);   // bit 16 (i / 4) + i % 4 is element i's key
 #pragma unroll
-      for (int i = 0; i < 16; i++) s[i] = bits >> (8 * (i >> 2) + (i & 3)) & 1 ? s[i] : -INFINITY;
-    };
-    // The reference follows the maximum only where a weight would pass 2^(8 + HEADROOM): in the first tiles, hardly ever later.
-    // fp16 weights start at 2^HEADROOM, so that small ones keep their bits.  top: of this lane's scores
-    auto settle = [&](float top) {
-      constexpr float HEADROOM = Mat<T>::EXPONENT == 0x7c00 ? 7.f : 0.f;
-      top = max_xor32(top) * a.scale;
-      if (__ballot(top > st.m + (8.f + HEADROOM)) != 0) {
-        const float m = fmaxf(st.m, top - HEADROOM), keep = st.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st.m - m);
-        st.m = m;
-        st.l *= keep;
-        scale_sums<D / 32>(st.o, keep);
+        for (int i = 0; i < 8; i++) s[n][i] = bits >> (16 * (i >> 2) + (i & 3)) & 1 ? s[n][i] : -INFINITY;
       }
     };
-    auto top_of = [&](const f32x16& s) {
-      float top = s[0];
+    // The reference of the exponents is the maximum of a row's first granule, and follows it only where a weight would pass
+    // 2^(8 + HEADROOM): hardly ever.  fp16 weights start at 2^HEADROOM, so that small ones keep their bits.  top: of this lane's scores
+    constexpr float HEADROOM = Mat<T>::EXPONENT == 0x7c00 ? 7.f : 0.f;
+    auto refer_to = [&](float (&top)[R]) {   // gives back in top what sums so far have to be multiplied by
 #pragma unroll
-      for (int i = 1; i < 16; i++) top = fmaxf(top, s[i]);
-      return top;
+      for (int n = 0; n < R; n++) {
+        const float m = fmaxf(st[n].m, max_xor32(max_xor16(top[n])) * a.scale - HEADROOM);
+        top[n] = st[n].m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st[n].m - m);
+        st[n].m = m;
+        st[n].shift = m == -INFINITY ? 0.f : -m;
+        st[n].l *= top[n];
+      }
     };
-    s16x8 pf[2];
-    auto weigh = [&](const f32x16& s, int i) {   // registers i and i + 1
-      const float m = st.m == -INFINITY ? 0.f : st.m;
+    auto settle = [&](float (&top)[R]) {
+      bool past = false, sums = false;
+#pragma unroll
+      for (int n = 0; n < R; n++) past |= top[n] * a.scale > st[n].m + (8.f + HEADROOM), sums |= st[n].m != -INFINITY;
+      if (__ballot(past) != 0) {
+        refer_to(top);
+        if (__ballot(sums) != 0) {   // (not in the first granule: code that is not reached is not fetched)
+#pragma unroll
+          for (int n = 0; n < R; n++) scale_sums<TILES>(st[n].o, top[n]);
+        }
+      }
+    };
+    // (The empty assembly holds what is made beside products there: the compiler moves it behind the next branch otherwise.)
+    unsigned pw[R][4];
+    auto weigh = [&](const f32x8 (&s)[R], int pair) {   // two scores of this lane, of 4 R
+      const int n = pair >> 2, i = pair & 3;
       T2 w;
-      w[0] = (T)__builtin_amdgcn_exp2f(fmaf(s[i], a.scale, -m));
-      w[1] = (T)__builtin_amdgcn_exp2f(fmaf(s[i + 1], a.scale, -m));
-      st.l = dot_ones(w, st.l);   // of what the product takes, so that rounding a dominant weight cancels
-      pf[i >> 3][i & 7] = __builtin_bit_cast(short, (T)w[0]);
-      pf[i >> 3][(i & 7) + 1] = __builtin_bit_cast(short, (T)w[1]);
+      w[0] = (T)__builtin_amdgcn_exp2f(fmaf(s[n][2 * i], a.scale, st[n].shift));
+      w[1] = (T)__builtin_amdgcn_exp2f(fmaf(s[n][2 * i + 1], a.scale, st[n].shift));
+      st[n].l = dot_ones(w, st[n].l);   // of what the product takes, so that rounding a dominant weight cancels
+      pw[n][i] = __builtin_bit_cast(unsigned, w);
+      asm volatile("" : "+v"(pw[n][i]), "+v"(st[n].l));
     };
-    auto sum_values = [&](auto beside) {
+    auto sum_values = [&](int stage, auto beside) {
+      s16x8 pf[R];
 #pragma unroll
-      for (int i = 0; i < PRODUCTS; i++) {
-        st.o[i >> 1] = Mat<T>::mfma(vf[i], pf[i & 1], st.o[i >> 1]);
+      for (int n = 0; n < R; n++) pf[n] = __builtin_bit_cast(s16x8, uint4{pw[n][0], pw[n][1], pw[n][2], pw[n][3]});
+#pragma unroll
+      for (int i = 0; i < TILES; i++) {
+        if (i + LEAD_V < TILES) read_values(stage, i + LEAD_V);
+#pragma unroll
+        for (int n = 0; n < R; n++) st[n].o[i] = Mat<T>::mfma(vf[i], pf[n], st[n].o[i]);
         beside(i);
+        __builtin_amdgcn_sched_barrier(0);
       }
     };
-    auto request_next = [&](int granule, int stage) {   // into the place of the stage in front of `stage`
-      none = none << 2 | (next1 < 0) << 1 | (next0 < 0);
-      if (granule + STAGES - 1 < g1) request(granule + STAGES - 1, stage == 0 ? STAGES - 1 : stage - 1, next0, next1);
+    auto maximum = [&](float (&top)[R], const f32x8 (&s)[R], int from, int to) {   // over scores from .. to - 1 of this lane's 8 R
+#pragma unroll
+      for (int i = 0; i < 8 * R; i += 2) {
+        if (i < from || i >= to) continue;
+        const float pair = fmaxf(s[i >> 3][i & 7], s[i >> 3][(i & 7) + 1]);
+        top[i >> 3] = (i & 7) == 0 ? pair : fmaxf(top[i >> 3], pair);
+        asm volatile("" : "+v"(top[i >> 3]));
+      }
     };
     // until a granule is there: AFTER granules behind it may be on their way, and all are waited for where the unit has fewer
     auto arrived = [&](int granule, auto after) {
-      if (granule + after < g1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(after * REQUESTS) : "memory");
+      if (AHEAD || granule + after < g1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(after * REQUESTS) : "memory");
       else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       __syncthreads();   // from every wave; and the granule before has been read by every wave
     };
-    auto next_pages = [&](int granule) { next0 = page_of(granule + STAGES, 0), next1 = page_of(granule + STAGES, 1); };
 
     int stage = 0;
     if constexpr (AHEAD) {
       // scores one granule ahead: their products run beside the exponentials of the granule whose values are summed next
       arrived(g0, std::integral_constant<int, STAGES - 2>());
-      f32x16 s = scores(0, [] {}, [](int) {});
+      f32x8 s[R], s_next[R];
+      float top[R];
+      scores(0, s, [](int) {});
       hide(s, g0, none >> (2 * (STAGES - 2)) & 3);
-      settle(top_of(s));
+      maximum(top, s, 0, 8 * R);
+      refer_to(top);
+#pragma unroll 1
       for (int granule = g0; granule < g1; granule++) {
         arrived(granule + 1, std::integral_constant<int, STAGES - 3>());
         clean_values(granule, stage, none >> (2 * (STAGES - 2)) & 3);
-        const int stage1 = stage + 1 == STAGES ? 0 : stage + 1;
-        f32x16 s_next = scores(stage1, [&] { request_next(granule, stage); }, [&](int i) {
-          read_values(stage, i);
+        const int stage1 = stage + 1 == STAGES ? 0 : stage + 1, wanted = granule + STAGES - 1;
+        next_pages();
+        const Quarter at = quarter_of(rw, in_unit(wanted), stage == 0 ? STAGES - 1 : stage - 1, page0, page1);
+        scores(stage1, s_next, [&](int i) {
+          first_values(stage, i);
 #pragma unroll
-          for (int j = i * 8 / PRODUCTS; j < (i + 1) * 8 / PRODUCTS; j++) weigh(s, 2 * j);
+          for (int j = i * QUARTER / STEPS; j < (i + 1) * QUARTER / STEPS; j++) request_kib(at, rw >= 2, j);
+#pragma unroll
+          for (int j = i * 4 * R / STEPS; j < (i + 1) * 4 * R / STEPS; j++) weigh(s, j);
         });
         if (granule + 1 < g1) hide(s_next, granule + 1, none >> (2 * (STAGES - 2)) & 3);
-        float top = s_next[0];
-        sum_values([&](int i) {
-#pragma unroll
-          for (int j = i * 16 / PRODUCTS; j < (i + 1) * 16 / PRODUCTS; j++) top = fmaxf(top, s_next[j]);
-          __builtin_amdgcn_sched_barrier(0);
-        });
+        sum_values(stage, [&](int i) { maximum(top, s_next, i * 8 * R / TILES, (i + 1) * 8 * R / TILES); });
+        next_entries(in_unit(wanted + 1));
         if (granule + 1 < g1) settle(top);
-        next_pages(granule);   // (reads that other reads would have to wait for, so: when there are none)
-        s = s_next;
+#pragma unroll
+        for (int n = 0; n < R; n++) s[n] = s_next[n];
         stage = stage1;
       }
     } else {
+      f32x8 s[R];
+      float top[R];
       for (int granule = g0; granule < g1; granule++) {
         arrived(granule, std::integral_constant<int, STAGES - 2>());
         clean_values(granule, stage, none >> (2 * (STAGES - 2)) & 3);
-        f32x16 s = scores(stage, [&] { request_next(granule, stage); }, [&](int i) { read_values(stage, i); });
+        const int wanted = granule + STAGES - 1;
+        next_pages();
+        if (wanted < g1) request(wanted, stage == 0 ? STAGES - 1 : stage - 1, page0, page1);
+        scores(stage, s, [&](int i) { first_values(stage, i); });
         hide(s, granule, none >> (2 * (STAGES - 1)) & 3);
-        settle(top_of(s));
+        maximum(top, s, 0, 8 * R);
+        settle(top);
 #pragma unroll
-        for (int i = 0; i < 16; i += 2) weigh(s, i);
-        sum_values([](int) {});
-        next_pages(granule);
+        for (int j = 0; j < 4 * R; j++) weigh(s, j);
+        sum_values(stage, [](int) {});
+        next_entries(in_unit(wanted + 1));
         stage = stage + 1 == STAGES ? 0 : stage + 1;
       }
     }
-    st.l = add_xor32(st.l);
-
-    if (!live) continue;
-    if (odd_from < g1) {
-      // rare: sums that such values are part of are what adding them makes of any number
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // nothing is on its way to the tiles any more
+#pragma unroll
+    for (int n = 0; n < R; n++) {
+      RowState<D>& row = st[n];
+      row.l = add_xor32(add_xor16(row.l));
+      if (!live[n]) continue;
+      if (odd_from < g1) {
+        // rare: sums that such values are part of are what adding them makes of any number
 #pragma unroll 1
-      for (int pos = odd_from * GRANULE; pos < min(total, g1 * GRANULE); pos++) {
-        const int j = pos - length, page = page_at(p, seq, pos >> shift);
-        const bool sees = j < 0 || (mask != nullptr ? (j >> 5) < a.mask_words && (mask[j >> 5] >> (j & 31) & 1) : j <= node);
-        if (!sees || page < 0) continue;
-        const T* row = reinterpret_cast<const T*>(pool_v) + page * p.page_stride + (pos & in_page) * p.token_stride + 4 * h;
+        for (int pos = odd_from * GRANULE; pos < min(total, g1 * GRANULE); pos++) {
+          const int j = pos - length, page = page_at(p, seq, pos >> shift);
+          const bool sees = j < 0 || (a.mask != nullptr ? (j >> 5) < a.mask_words && (mask[n][j >> 5] >> (j & 31) & 1) : j <= node[n]);
+          if (!sees || page < 0) continue;
+          const T* v_row = reinterpret_cast<const T*>(pool_v) + page * p.page_stride + (pos & in_page) * p.token_stride + 4 * quad;
 #pragma unroll
-        for (int c = 0; c < D / 8; c++) {
-          const T4 v = *reinterpret_cast<const T4*>(row + c * 8);
+          for (int b = 0; b < TILES; b++) {
+            const T4 v = *reinterpret_cast<const T4*>(v_row + b * 16);
 #pragma unroll
-          for (int i = 0; i < 4; i++) {
-            const float x = (float)v[i];
-            st.o[c >> 2][(c & 3) * 4 + i] += x - x == 0.f ? 0.f : x;
+            for (int i = 0; i < 4; i++) {
+              const float x = (float)v[i];
+              row.o[b][i] += x - x == 0.f ? 0.f : x;
+            }
           }
         }
       }
-    }
-    if (g0 == 0 && g1 == granules) {
-      const float inv = st.l == 0.f ? 0.f : 1.0f / st.l;
-      T* out = reinterpret_cast<T*>(a.out) + (rows.x + node) * a.out_row_stride + head * a.out_head_stride;
+      if (g0 == 0 && g1 == granules) {
+        const float inv = row.l == 0.f ? 0.f : 1.0f / row.l;
+        T* out = reinterpret_cast<T*>(a.out) + (rows.x + node[n]) * a.out_row_stride + head[n] * a.out_head_stride;
 #pragma unroll
-      for (int b = 0; b < D / 32; b++) {
-#pragma unroll
-        for (int i = 0; i < 16; i += 4) {
+        for (int b = 0; b < TILES; b++) {
           T4 w;
 #pragma unroll
-          for (int c = 0; c < 4; c++) w[c] = (T)(st.o[b][i + c] * inv);
-          *reinterpret_cast<T4*>(out + b * 32 + 2 * i + 4 * h) = w;
+          for (int i = 0; i < 4; i++) w[i] = (T)(row.o[b][i] * inv);
+          *reinterpret_cast<T4*>(out + b * 16 + 4 * quad) = w;
         }
+      } else {
+        const size_t slot = ((size_t)mine_run * 2 + (g0 == 0)) * ROWS + (rw * R + n) * 16 + kkey;
+        float* out = a.part_o + slot * D;
+#pragma unroll
+        for (int b = 0; b < TILES; b++) *reinterpret_cast<f32x4*>(out + b * 16 + 4 * quad) = row.o[b];
+        if (quad == 0) a.part_ml[slot] = make_float2(row.m, row.l);
       }
-    } else {
-      const size_t slot = ((size_t)mine_run * 2 + (g0 == 0)) * ROWS + rw * 32 + (lane & 31);
-      float* out = a.part_o + slot * D;
-#pragma unroll
-      for (int b = 0; b < D / 32; b++) {
-#pragma unroll
-        for (int i = 0; i < 16; i += 4) {
-          f32x4 w;
-#pragma unroll
-          for (int c = 0; c < 4; c++) w[c] = st.o[b][i + c];
-          *reinterpret_cast<f32x4*>(out + b * 32 + 2 * i + 4 * h) = w;
-        }
-      }
-      if (h == 0) a.part_ml[slot] = make_float2(st.m, st.l);
     }
   }
 }
 
 // The rows of units that several blocks had a part in: sum_z 2^(m_z - m) o_z / sum_z 2^(m_z - m) l_z, in the order of the keys.  WPR
 // waves share out a row's parts, D / 64 numbers per lane: 8 where units are so few that each has many, one where they are many.
-template <class T, int D, int RW, int WPR>
+template <class T, int D, int RW, int R, int WPR>
 __global__ __launch_bounds__(512) void tree_merge_kernel(TreeArgs a) {
-  constexpr int ROWS = 32 * RW, PER = D / 64;
+  constexpr int ROWS = 16 * R * RW, PER = D / 64;
   typedef float Vec __attribute__((ext_vector_type(PER)));
   typedef T VecT __attribute__((ext_vector_type(PER)));
   const pi0_pages& p = a.p;
@@ -637,10 +713,10 @@ __global__ __launch_bounds__(512) void tree_merge_kernel(TreeArgs a) {
 struct Space {
   size_t part_ml, upto, cut, bytes;   // part_o lies in front
 };
-template <int D, int RW>
+template <int D, int RW, int R>
 Space space_of(const pi0_pages& p) {
   Space s;
-  const size_t slots = (size_t)Shape<D, RW>::BLOCKS * 2 * 32 * RW;
+  const size_t slots = (size_t)Shape<D, RW, R>::BLOCKS * 2 * 16 * R * RW;
   s.part_ml = slots * D * sizeof(float);
   s.upto = s.part_ml + slots * sizeof(float2);
   s.cut = s.upto + (size_t)p.n_seqs * sizeof(int);
@@ -648,59 +724,60 @@ Space space_of(const pi0_pages& p) {
   return s;
 }
 
-// 32, 64, 128 or 256 rows per tile, the least that all rows of a sequence and key/value head fit: its keys are read once then.
-// (256 rows of 256 d do not fit the registers of two waves per SIMD.)
-template <int D>
-constexpr int most_waves() { return D == 256 ? 4 : 8; }
-template <int D>
-int row_waves(int max_rows, int group) {
-  const int rows = max_rows * group;
-  return rows <= 32 ? 1 : rows <= 64 ? 2 : rows <= 128 ? 4 : most_waves<D>();
+// f<RW, R>(): 16, 32, 64 or 128 rows per tile, the least that all rows of a sequence and key/value head fit - its keys are read once
+// then -, and as many as the registers hold where they are more.
+template <int D, class F>
+auto with_rows(int rows, F f) {
+  using std::integral_constant;
+  constexpr integral_constant<int, 1> one;
+  constexpr integral_constant<int, 2> two;
+  constexpr integral_constant<int, 4> four;
+  if (rows <= 16) return f(one, one);
+  if (rows <= 32) return f(two, one);
+  if (rows <= 64) return f(four, one);
+  return f(four, two);
+}
+template <class F>
+auto with_dim(int head_dim, F f) {
+  if (head_dim == 64) return f(std::integral_constant<int, 64>());
+  if (head_dim == 128) return f(std::integral_constant<int, 128>());
+  return f(std::integral_constant<int, 256>());
 }
 
-template <int D>
 Space space_of(const pi0_pages& p, int heads, int max_rows) {
-  const int rw = row_waves<D>(max_rows, heads / p.kv_heads);
-  return rw == 1 ? space_of<D, 1>(p) : rw == 2 ? space_of<D, 2>(p) : rw == 4 ? space_of<D, 4>(p) : space_of<D, most_waves<D>()>(p);
-}
-Space space_of(const pi0_pages& p, int heads, int max_rows) {
-  return p.head_dim == 64 ? space_of<64>(p, heads, max_rows) : p.head_dim == 128 ? space_of<128>(p, heads, max_rows) : space_of<256>(p, heads, max_rows);
+  return with_dim(p.head_dim, [&](auto d) {
+    return with_rows<d>(max_rows * (heads / p.kv_heads), [&](auto rw, auto r) { return space_of<d, rw, r>(p); });
+  });
 }
 
-template <class T, int D, int RW>
-void launch(hipStream_t s, TreeArgs& a, char* ws) {
-  const Space at = space_of<D, RW>(a.p);
-  a.part_o = reinterpret_cast<float*>(ws);
-  a.part_ml = reinterpret_cast<float2*>(ws + at.part_ml);
-  a.upto = reinterpret_cast<int*>(ws + at.upto);
-  a.cut = reinterpret_cast<Cut*>(ws + at.cut);
-  hipLaunchKernelGGL((tree_attention_kernel<T, D, RW>), dim3(Shape<D, RW>::BLOCKS), dim3(64 * RW), 0, s, a);
-  const int rows = a.max_rows * a.group, units = a.p.n_seqs * a.p.kv_heads * div_up(rows, 32 * RW);
-  if (units <= Shape<D, RW>::BLOCKS / 16)
-    hipLaunchKernelGGL((tree_merge_kernel<T, D, RW, 8>), dim3(rows, a.p.kv_heads, a.p.n_seqs), dim3(512), 0, s, a);
-  else
-    hipLaunchKernelGGL((tree_merge_kernel<T, D, RW, 1>), dim3(div_up(rows, 8), a.p.kv_heads, a.p.n_seqs), dim3(512), 0, s, a);
-}
-template <class T, int D>
-void launch(hipStream_t s, TreeArgs& a, char* ws) {
-  const int rw = row_waves<D>(a.max_rows, a.group);
-  if (rw == 1) launch<T, D, 1>(s, a, ws);
-  else if (rw == 2) launch<T, D, 2>(s, a, ws);
-  else if (rw == 4) launch<T, D, 4>(s, a, ws);
-  else launch<T, D, most_waves<D>()>(s, a, ws);
-}
 template <class T>
 void launch(hipStream_t s, TreeArgs& a, char* ws) {
-  if (a.p.head_dim == 64) launch<T, 64>(s, a, ws);
-  else if (a.p.head_dim == 128) launch<T, 128>(s, a, ws);
-  else launch<T, 256>(s, a, ws);
+  with_dim(a.p.head_dim, [&](auto d) {
+    const int rows = a.max_rows * a.group;
+    with_rows<d>(rows, [&](auto rw, auto r) {
+      constexpr int D = d, RW = rw, R = r, BLOCKS = Shape<D, RW, R>::BLOCKS;
+      const Space at = space_of<D, RW, R>(a.p);
+      a.part_o = reinterpret_cast<float*>(ws);
+      a.part_ml = reinterpret_cast<float2*>(ws + at.part_ml);
+      a.upto = reinterpret_cast<int*>(ws + at.upto);
+      a.cut = reinterpret_cast<Cut*>(ws + at.cut);
+      hipLaunchKernelGGL((tree_attention_kernel<T, D, RW, R>), dim3(BLOCKS), dim3(64 * RW), 0, s, a);
+      const int units = a.p.n_seqs * a.p.kv_heads * div_up(rows, 16 * R * RW);
+      if (units <= BLOCKS / 16)
+        hipLaunchKernelGGL((tree_merge_kernel<T, D, RW, R, 8>), dim3(rows, a.p.kv_heads, a.p.n_seqs), dim3(512), 0, s, a);
+      else
+        hipLaunchKernelGGL((tree_merge_kernel<T, D, RW, R, 1>), dim3(div_up(rows, 8), a.p.kv_heads, a.p.n_seqs), dim3(512), 0, s, a);
+      return 0;
+    });
+    return 0;
+  });
 }
 
 bool args_ok(const pi0_pages* p, int heads, int n_rows, int max_rows) {
   if (!pages_ok(p) || heads < 1 || heads > 1024 || heads % p->kv_heads != 0) return false;
   if (n_rows < 1 || n_rows > 1 << 24 || max_rows < 1 || max_rows > 1024 || max_rows > n_rows) return false;
   // the line of all units' granules is counted in 31 bits
-  const int64_t tiles = div_up(max_rows * (heads / p->kv_heads), 32), granules = div_up(p->max_pages * p->page_tokens, GRANULE) + START;
+  const int64_t tiles = div_up(max_rows * (heads / p->kv_heads), 16), granules = div_up(p->max_pages * p->page_tokens, GRANULE) + START;
   return (int64_t)p->n_seqs * p->kv_heads * tiles * granules < (int64_t)1 << 30;
 }
 
