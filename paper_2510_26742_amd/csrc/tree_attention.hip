@@ -99,7 +99,7 @@ struct TreeArgs {
   // workspace
   int* upto;             // [n_seqs] where a sequence's share of the line ends
   Cut* cut;
-  float* part_o;         // [runs][2][rows of a tile][head_dim]
+  f32x4* part_o;         // [runs][2][rows of a tile / 16][head_dim / 16][64]: as a wave holds them
   float2* part_ml;       // [runs][2][rows of a tile]: reference of the exponents, sum of the weights
 };
 
@@ -192,7 +192,7 @@ template <class T, int D, int RW, int R>
 __global__ __launch_bounds__(64 * RW, RW >= 4 && (D < 256 || R == 1) ? 2 : 1) void tree_attention_kernel(TreeArgs a) {
   constexpr int STAGES = Shape<D, RW, R>::STAGES, BLOCKS = Shape<D, RW, R>::BLOCKS, ROWS = 16 * R * RW;
   constexpr int PIECES = D / 8, TILE = 32 * D * 2, PARTS = TILE / 1024, REQUESTS = 2 * PARTS / RW, KEYS_PER_REQUEST = 512 / D;
-  constexpr bool AHEAD = R > 1;
+  constexpr int AHEAD = R > 1;
   constexpr int STEPS = D / 32, TILES = D / 16;   // of 32 d that scores are summed over, of 16 d that sums are kept for
   static_assert(REQUESTS >= 1 && STAGES >= (AHEAD ? 3 : 2) && (!AHEAD || RW == 4) && (STAGES - 2) * REQUESTS < 64, "the wait counter holds what is in flight");
   typedef T T2 __attribute__((ext_vector_type(2)));
@@ -310,6 +310,18 @@ __global__ __launch_bounds__(64 * RW, RW >= 4 && (D < 256 || R == 1) ? 2 : 1) vo
       if (g0 >= g1) continue;   // the run ends in front of the unit's first granule
     }
 
+    // The pages of the first granules.  With AHEAD the last granule is requested again where there is none behind it, into a stage that
+    // nobody reads any more: as many requests are on their way at the end as anywhere, and no branch parts the products.
+    int entry0, entry1, entries[STAGES - 1][2];
+    auto in_unit = [&](int granule) { return AHEAD ? min(granule, g1 - 1) : granule; };
+    auto next_entries = [&](int granule) {
+      entry0 = entry_at(p, seq, granule * GRANULE >> shift), entry1 = entry_at(p, seq, (granule * GRANULE + 16) >> shift);
+    };
+#pragma unroll
+    for (int i = 0; i < STAGES - 1; i++) {
+      next_entries(in_unit(g0 + i));
+      entries[i][0] = entry0, entries[i][1] = entry1;
+    }
     // this lane's rows: token and head
     int node[R], head[R];
     bool live[R];
@@ -371,7 +383,7 @@ __global__ __launch_bounds__(64 * RW, RW >= 4 && (D < 256 || R == 1) ? 2 : 1) vo
     for (int n = 0; n < R; n++) {
 #pragma unroll
       for (int b = 0; b < TILES; b++) {
-        st[n].o[b] = f32x4{};
+        st[n].o[b] = Mat<T>::mfma(s16x8{}, s16x8{}, f32x4{});   // (zeros, 8 bytes of code for 4 registers)
         asm volatile("" : "+a"(st[n].o[b]));   // (where they stay; the compiler would move them back and forth)
       }
       st[n].m = -INFINITY;
@@ -381,30 +393,16 @@ __global__ __launch_bounds__(64 * RW, RW >= 4 && (D < 256 || R == 1) ? 2 : 1) vo
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // from here on only the tiles' requests are in flight
     __syncthreads();                                   // what was in the tiles has been read
     unsigned none = 0;   // two bits per granule, the latest requested lowest: its first, last 16 keys are on no page
-    int entry0, entry1, page0, page1;
-    auto next_entries = [&](int granule) {
-      entry0 = entry_at(p, seq, granule * GRANULE >> shift), entry1 = entry_at(p, seq, (granule * GRANULE + 16) >> shift);
-    };
+    int page0, page1;
     auto next_pages = [&] {
       page0 = (unsigned)entry0 < (unsigned)p.n_pages ? entry0 : -1, page1 = (unsigned)entry1 < (unsigned)p.n_pages ? entry1 : -1;
       none = none << 2 | (page1 < 0) << 1 | (page0 < 0);
     };
-    // With AHEAD the last granule is requested again where there is none behind it, into a stage that nobody reads any more: as
-    // many requests are on their way at the end as anywhere, and no branch parts the products.
-    auto in_unit = [&](int granule) { return AHEAD ? min(granule, g1 - 1) : granule; };
-    {
-      int entries[STAGES - 1][2];
 #pragma unroll
-      for (int i = 0; i < STAGES - 1; i++) {
-        next_entries(in_unit(g0 + i));
-        entries[i][0] = entry0, entries[i][1] = entry1;
-      }
-#pragma unroll
-      for (int i = 0; i < STAGES - 1; i++) {
-        entry0 = entries[i][0], entry1 = entries[i][1];
-        next_pages();
-        if (AHEAD || g0 + i < g1) request(in_unit(g0 + i), i, page0, page1);
-      }
+    for (int i = 0; i < STAGES - 1; i++) {
+      entry0 = entries[i][0], entry1 = entries[i][1];
+      next_pages();
+      if (AHEAD || g0 + i < g1) request(in_unit(g0 + i), i, page0, page1);
     }
     next_entries(in_unit(g0 + STAGES - 1));
 
@@ -557,7 +555,20 @@ __global__ __launch_bounds__(64 * RW, RW >= 4 && (D < 256 || R == 1) ? 2 : 1) vo
     };
 
     int stage = 0;
-    if constexpr (AHEAD) {
+    if (RW > 1 && row_tile * ROWS + rw * R * 16 >= rows.y * a.group) {
+      // a wave without rows: its part of the requests, and what all waves do together
+      if (AHEAD) arrived(g0, std::integral_constant<int, STAGES - 2>());
+#pragma unroll 1
+      for (int granule = g0; granule < g1; granule++) {
+        arrived(granule + AHEAD, std::integral_constant<int, STAGES - 2 - AHEAD>());
+        clean_values(granule, stage, none >> (2 * (STAGES - 2)) & 3);
+        const int wanted = granule + STAGES - 1;
+        next_pages();
+        if (AHEAD || wanted < g1) request(in_unit(wanted), stage == 0 ? STAGES - 1 : stage - 1, page0, page1);
+        next_entries(in_unit(wanted + 1));
+        stage = stage + 1 == STAGES ? 0 : stage + 1;
+      }
+    } else if constexpr (AHEAD) {
       // scores one granule ahead: their products run beside the exponentials of the granule whose values are summed next
       arrived(g0, std::integral_constant<int, STAGES - 2>());
       f32x8 s[R], s_next[R];
@@ -644,30 +655,28 @@ __global__ __launch_bounds__(64 * RW, RW >= 4 && (D < 256 || R == 1) ? 2 : 1) vo
           *reinterpret_cast<T4*>(out + b * 16 + 4 * quad) = w;
         }
       } else {
-        const size_t slot = ((size_t)mine_run * 2 + (g0 == 0)) * ROWS + (rw * R + n) * 16 + kkey;
-        float* out = a.part_o + slot * D;
+        const size_t set = ((size_t)mine_run * 2 + (g0 == 0)) * (ROWS / 16) + rw * R + n;
 #pragma unroll
-        for (int b = 0; b < TILES; b++) *reinterpret_cast<f32x4*>(out + b * 16 + 4 * quad) = row.o[b];
-        if (quad == 0) a.part_ml[slot] = make_float2(row.m, row.l);
+        for (int b = 0; b < TILES; b++) a.part_o[(set * TILES + b) * 64 + lane] = row.o[b];
+        if (quad == 0) a.part_ml[set * 16 + kkey] = make_float2(row.m, row.l);
       }
     }
   }
 }
 
-// The rows of units that several blocks had a part in: sum_z 2^(m_z - m) o_z / sum_z 2^(m_z - m) l_z, in the order of the keys.  WPR
-// waves share out a row's parts, D / 64 numbers per lane: 8 where units are so few that each has many, one where they are many.
+// The rows of units that several blocks had a part in: sum_z 2^(m_z - m) o_z / sum_z 2^(m_z - m) l_z, in the order of the keys.  A wave
+// has 16 d of 16 rows, as the partial results lie; WPR waves share out the parts: 8 where units are so few that each has many.
 template <class T, int D, int RW, int R, int WPR>
 __global__ __launch_bounds__(512) void tree_merge_kernel(TreeArgs a) {
-  constexpr int ROWS = 16 * R * RW, PER = D / 64;
-  typedef float Vec __attribute__((ext_vector_type(PER)));
-  typedef T VecT __attribute__((ext_vector_type(PER)));
+  constexpr int ROWS = 16 * R * RW, TILES = D / 16, BATCH = 4;
+  typedef T T4 __attribute__((ext_vector_type(4)));
   const pi0_pages& p = a.p;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, share = wave % WPR;
-  const int r = blockIdx.x * (8 / WPR) + wave / WPR, kv_head = blockIdx.y, seq = blockIdx.z;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, share = wave % WPR, kkey = lane & 15, quad = lane >> 4;
+  const int item = blockIdx.x * (8 / WPR) + wave / WPR, set = item / TILES, tile = item % TILES, kv_head = blockIdx.y, seq = blockIdx.z;
   const int2 rows = rows_of(a.row_start, seq, a.n_rows, a.max_rows);
-  if (r >= rows.y * a.group) return;   // (with WPR == 8 all of a block's waves)
+  if (set * 16 >= rows.y * a.group) return;   // (with WPR == 8 all of a block's waves)
   const int total = min(length_of(p, seq) + rows.y, p.max_pages * p.page_tokens);
-  const int granules = div_up(total, GRANULE), row_tiles = div_up(rows.y * a.group, ROWS), row_tile = r / ROWS;
+  const int granules = div_up(total, GRANULE), row_tiles = div_up(rows.y * a.group, ROWS), row_tile = set / (ROWS / 16);
   const Cut cut = *a.cut;
   const int before = (seq > 0 ? a.upto[seq - 1] : 0) + kv_head * row_tiles * cut.length(granules);
   int run0, parts, step = 1;   // the runs that had a part
@@ -678,36 +687,55 @@ __global__ __launch_bounds__(512) void tree_merge_kernel(TreeArgs a) {
     run0 = first / cut.run, parts = (first + granules - 1) / cut.run - run0 + 1;
   }
   if (parts < 2) return;
-  auto slot_of = [&](int part) { return ((size_t)(run0 + part * step) * 2 + (part == 0)) * ROWS + r % ROWS; };
-  float m = -INFINITY;
-  for (int i = lane; i < parts; i += 64) m = fmaxf(m, a.part_ml[slot_of(i)].x);
-  for (int i = 32; i > 0; i >>= 1) m = fmaxf(m, __shfl_xor(m, i));
-  const float safe = m == -INFINITY ? 0.f : m;
-  Vec o = {};
-  float l = 0.f;
-#pragma unroll 4
-  for (int i = share; i < parts; i += WPR) {
-    const size_t slot = slot_of(i);
-    const float2 ml = a.part_ml[slot];
-    const float c = __builtin_amdgcn_exp2f(ml.x - safe);
-    o += c * *reinterpret_cast<const Vec*>(a.part_o + slot * D + lane * PER);
-    l += c * ml.y;
+  // this wave's parts, each row against the maximum of its own so far; what a row that is not there holds stays in its lanes
+  f32x4 o = {};
+  float m = -INFINITY, l = 0.f;
+#pragma unroll 1
+  for (int part = share; part < parts; part += BATCH * WPR) {
+    float2 ml[BATCH];
+    f32x4 v[BATCH];
+#pragma unroll
+    for (int i = 0; i < BATCH; i++) {
+      const int z = part + i * WPR;
+      const size_t from = ((size_t)(run0 + min(z, parts - 1) * step) * 2 + (z == 0)) * (ROWS / 16) + set % (ROWS / 16);
+      ml[i] = a.part_ml[from * 16 + kkey];
+      v[i] = a.part_o[(from * TILES + tile) * 64 + lane];
+      if (z >= parts) ml[i].x = -INFINITY, v[i] = f32x4{};
+    }
+    float top = m;
+#pragma unroll
+    for (int i = 0; i < BATCH; i++) top = fmaxf(top, ml[i].x);
+    const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+    o *= keep, l *= keep, m = top;
+#pragma unroll
+    for (int i = 0; i < BATCH; i++) {
+      const float c = ml[i].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[i].x - m);
+      o += c * v[i], l += c * ml[i].y;
+    }
   }
   if constexpr (WPR > 1) {
-    __shared__ float s_l[WPR];
-    __shared__ Vec s_o[WPR][64];
-    if (lane == 0) s_l[share] = l;
+    __shared__ float2 s_ml[WPR][16];
+    __shared__ f32x4 s_o[WPR][64];
+    if (quad == 0) s_ml[share][kkey] = make_float2(m, l);
     s_o[share][lane] = o;
     __syncthreads();
     if (share != 0) return;
-    for (int w = 1; w < WPR; w++) o += s_o[w][lane], l += s_l[w];
+    for (int w = 1; w < WPR; w++) m = fmaxf(m, s_ml[w][kkey].x);
+    o = f32x4{}, l = 0.f;
+    for (int w = 0; w < WPR; w++) {
+      const float2 ml = s_ml[w][kkey];
+      const float c = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - m);
+      o += c * s_o[w][lane], l += c * ml.y;
+    }
   }
+  const int r = set * 16 + kkey;
+  if (r >= rows.y * a.group) return;
   const float inv = l == 0.f ? 0.f : 1.0f / l;
   const int node = r / a.group, head = kv_head * a.group + r - node * a.group;
-  VecT w;
+  T4 w;
 #pragma unroll
-  for (int i = 0; i < PER; i++) w[i] = (T)(o[i] * inv);
-  *reinterpret_cast<VecT*>(reinterpret_cast<T*>(a.out) + (rows.x + node) * a.out_row_stride + head * a.out_head_stride + lane * PER) = w;
+  for (int i = 0; i < 4; i++) w[i] = (T)(o[i] * inv);
+  *reinterpret_cast<T4*>(reinterpret_cast<T*>(a.out) + (rows.x + node) * a.out_row_stride + head * a.out_head_stride + tile * 16 + 4 * quad) = w;
 }
 
 struct Space {
@@ -757,16 +785,17 @@ void launch(hipStream_t s, TreeArgs& a, char* ws) {
     with_rows<d>(rows, [&](auto rw, auto r) {
       constexpr int D = d, RW = rw, R = r, BLOCKS = Shape<D, RW, R>::BLOCKS;
       const Space at = space_of<D, RW, R>(a.p);
-      a.part_o = reinterpret_cast<float*>(ws);
+      a.part_o = reinterpret_cast<f32x4*>(ws);
       a.part_ml = reinterpret_cast<float2*>(ws + at.part_ml);
       a.upto = reinterpret_cast<int*>(ws + at.upto);
       a.cut = reinterpret_cast<Cut*>(ws + at.cut);
       hipLaunchKernelGGL((tree_attention_kernel<T, D, RW, R>), dim3(BLOCKS), dim3(64 * RW), 0, s, a);
       const int units = a.p.n_seqs * a.p.kv_heads * div_up(rows, 16 * R * RW);
+      const int items = div_up(rows, 16) * (D / 16);   // of 16 rows and 16 d
       if (units <= BLOCKS / 16)
-        hipLaunchKernelGGL((tree_merge_kernel<T, D, RW, R, 8>), dim3(rows, a.p.kv_heads, a.p.n_seqs), dim3(512), 0, s, a);
+        hipLaunchKernelGGL((tree_merge_kernel<T, D, RW, R, 8>), dim3(items, a.p.kv_heads, a.p.n_seqs), dim3(512), 0, s, a);
       else
-        hipLaunchKernelGGL((tree_merge_kernel<T, D, RW, R, 1>), dim3(div_up(rows, 8), a.p.kv_heads, a.p.n_seqs), dim3(512), 0, s, a);
+        hipLaunchKernelGGL((tree_merge_kernel<T, D, RW, R, 1>), dim3(div_up(items, 8), a.p.kv_heads, a.p.n_seqs), dim3(512), 0, s, a);
       return 0;
     });
     return 0;
