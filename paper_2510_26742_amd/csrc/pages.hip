@@ -62,6 +62,7 @@ struct Move {
   int held;   // pages of the list as it was
 };
 // workspace: moves [n_seqs], the lists as they were [n_seqs][max_pages], the free pages that are handed out [n_pages]
+constexpr int SHARED = 1 << 30;   // in an entry of a list as it was: others hold the page too, and it is replaced
 struct PlanSpace {
   Move* moves;
   int* before;
@@ -93,13 +94,14 @@ __device__ __forceinline__ int lanes_below(unsigned long long mask) {
   return __builtin_amdgcn_mbcnt_hi((unsigned)(mask >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)mask, 0));
 }
 
-// pages in front of a sequence's list (by a whole wave)
-__device__ int pages_held(const pi0_pages& p, int seq, int lane) {
-  for (int at = 0; at < p.max_pages; at += 64) {
-    const unsigned long long none = __ballot(page_at(p, seq, at + lane) < 0);
+// pages in front of a sequence's list (by a whole wave, each lane of which has read its entry of the first 64)
+__device__ int pages_held(const pi0_pages& p, int seq, int lane, int entry) {
+  for (int at = 0;; entry = page_at(p, seq, at + lane)) {
+    const unsigned long long none = __ballot(entry < 0);
     if (none != 0) return min(p.max_pages, at + __ffsll(none) - 1);
+    at += 64;
+    if (at >= p.max_pages) return p.max_pages;
   }
-  return p.max_pages;
 }
 
 // exclusive prefix sum of `mine` over the block's threads; *total gets the sum.  sums: PLAN_WAVES ints of shared memory
@@ -146,26 +148,32 @@ struct PlanArgs {
 
 // For every sequence that takes part:  [first, last) of its list may hold pages that others hold too and that rows are written
 // to - those are replaced -, the list has `want` pages afterwards, of which it holds `held` now.  reserve: want >= held,
-// compact: want <= held.  Reading a list costs a trip to memory per 64 entries, so what one block does for 1024 sequences of
-// some tens of pages each is a few us; the free pages cost one trip per 1024 reference counts until enough are found.
+// compact: want <= held.  What bounds it is trips to memory (0.6 us each) and 16 waves for all sequences, so: numbers
+// that all sequences have are read at once, a list and the positions that it keeps in one trip, reference counts in a second, and what
+// was found is left in the workspace for the second half.  The free pages cost one trip per 1024 reference counts until enough are found.
 template <int KIND>
 __global__ __launch_bounds__(PLAN_THREADS) void pages_plan_kernel(PlanArgs a) {
   const pi0_pages& p = a.p;
-  __shared__ int s_need[MAX_SEQS], s_first[MAX_SEQS], s_last[MAX_SEQS], s_held[MAX_SEQS], s_want[MAX_SEQS];
+  __shared__ int s_need[MAX_SEQS], s_first[MAX_SEQS], s_last[MAX_SEQS], s_held[MAX_SEQS], s_want[MAX_SEQS], s_length[MAX_SEQS], s_n[MAX_SEQS];
   __shared__ int s_sums[PLAN_WAVES], s_bad;
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
   if (t == 0) s_bad = 0;
+  if (t < p.n_seqs) {
+    s_n[t] = KIND == PLAN_RESERVE ? a.extra[t] : a.n_keep[t];
+    s_length[t] = p.d_length[t];
+    s_first[t] = KIND == PLAN_COMPACT && a.start != nullptr ? a.start[t] : s_length[t];
+  }
   __syncthreads();
   for (int s = wave; s < p.n_seqs; s += PLAN_WAVES) {
-    const int n = KIND == PLAN_RESERVE ? a.extra[s] : a.n_keep[s];
+    const int n = s_n[s], length = s_length[s];
     int need = 0, first = 0, last = 0, held = 0, want = -1;   // want < 0: the sequence stays as it is
     Move m = {0, 0, 0, 0};
     if (n >= 0) {
-      held = pages_held(p, s, lane);
-      const int room = held * p.page_tokens, length = p.d_length[s];
-      bool bad = length < 0 || length > room;
+      const int entry = page_at(p, s, lane);
+      bool bad = length < 0;
       if (KIND == PLAN_RESERVE) {
-        bad |= (int64_t)length + n > (int64_t)p.max_pages * p.page_tokens;
+        held = pages_held(p, s, lane, entry);
+        bad |= length > held * p.page_tokens || (int64_t)length + n > (int64_t)p.max_pages * p.page_tokens;
         if (!bad) {
           want = max(held, div_up(length + n, p.page_tokens));
           first = length / p.page_tokens;
@@ -173,31 +181,47 @@ __global__ __launch_bounds__(PLAN_THREADS) void pages_plan_kernel(PlanArgs a) {
           m = {first * p.page_tokens, length, length, held};   // the committed rows of the first replaced page, if it is replaced
         }
       } else {
-        const int start = a.start != nullptr ? a.start[s] : length;
+        const int start = s_first[s];
         bad |= n > a.keep_stride || start < 0 || start > length;
+        int moved = n, furthest = -1;
         if (!bad) {
+          constexpr int DEEP = 8;   // in flight
           const int* keep = a.keep + (size_t)s * a.keep_stride;
-          int moved = n;
-          for (int i = lane; i < n; i += 64) {
-            const int k = keep[i];
-            bad |= k < 0 || (i > 0 && k <= keep[i - 1]) || (int64_t)start + k >= room;
-            if (k != i) moved = min(moved, i);
+          for (int at = lane; at < n; at += 64 * DEEP) {
+            int k[DEEP], in_front[DEEP];
+#pragma unroll
+            for (int j = 0; j < DEEP; j++) k[j] = keep[min(at + 64 * j, n - 1)], in_front[j] = keep[max(min(at + 64 * j, n - 1) - 1, 0)];
+#pragma unroll
+            for (int j = 0; j < DEEP; j++) {
+              const int i = min(at + 64 * j, n - 1);
+              bad |= k[j] < 0 || (i > 0 && k[j] <= in_front[j]);
+              if (k[j] != i) moved = min(moved, i);
+              furthest = max(furthest, k[j]);
+            }
           }
-          bad = __ballot(bad) != 0;
-          moved = wave_min(moved);
-          if (!bad) {
-            const int begin = start + moved, end = start + n;
-            want = div_up(end, p.page_tokens);
-            first = begin / p.page_tokens;
-            last = begin < end ? want : first;
-            m = {begin, end, start, held};
-          }
+        }
+        held = pages_held(p, s, lane, entry);
+        bad |= length > held * p.page_tokens || (furthest >= 0 && (int64_t)start + furthest >= (int64_t)held * p.page_tokens);
+        bad = __ballot(bad) != 0;
+        moved = wave_min(moved);
+        if (!bad) {
+          const int begin = start + moved, end = start + n;
+          want = div_up(end, p.page_tokens);
+          first = begin / p.page_tokens;
+          last = begin < end ? want : first;
+          m = {begin, end, start, held};
         }
       }
       if (bad) {
         s_bad = 1;
       } else {
-        for (int i = first + lane; i < last; i += 64) need += p.d_refs[page_at(p, s, i)] > 1;
+        int* before = a.ws.before + (size_t)s * p.max_pages;
+        for (int i = lane; i < held; i += 64) {
+          const int page = i < 64 ? entry : page_at(p, s, i);
+          const bool shared = i >= first && i < last && p.d_refs[max(page, 0)] > 1;
+          before[i] = shared ? page | SHARED : page;
+          need += shared;
+        }
         need = wave_sum(need) + max(0, want - held);
       }
     }
@@ -225,48 +249,40 @@ __global__ __launch_bounds__(PLAN_THREADS) void pages_plan_kernel(PlanArgs a) {
   }
   if (t < p.n_seqs) s_need[t] = base;   // from here on: the sequence's place among the free pages
   __syncthreads();
-  // lists, reference counts of pages that were free; which pages are shared is still what it was above
+  // lists and reference counts
+  auto handed_out = [&](int rank) { return rank < total ? a.ws.free_pages[rank] : -1; };
   for (int s = wave; s < p.n_seqs; s += PLAN_WAVES) {
     const int want = s_want[s], held = s_held[s], first = s_first[s], last = s_last[s];
     if (want < 0) continue;
     int* list = p.d_table + (size_t)s * p.max_pages;
-    int* before = a.ws.before + (size_t)s * p.max_pages;
-    for (int i = lane; i < held; i += 64) before[i] = list[i];
+    const int* before = a.ws.before + (size_t)s * p.max_pages;
     int next = s_need[s];
     bool first_replaced = false;
     for (int at = first; at < last; at += 64) {
-      const int i = at + lane;
-      const int page = i < last ? page_at(p, s, i) : -1;
-      const bool shared = page >= 0 && p.d_refs[page] > 1;
+      const int i = at + lane, entry = i < last ? before[i] : 0;
+      const bool shared = (entry & SHARED) != 0;
       const unsigned long long mask = __ballot(shared);
-      if (shared) take(p, list + i, a.ws.free_pages[next + lanes_below(mask)]);
+      if (shared) {
+        take(p, list + i, handed_out(next + lanes_below(mask)));
+        release(p, entry & ~SHARED);
+      }
       if (at == first) first_replaced = (mask & 1) != 0;
       next += __popcll(mask);
     }
-    for (int i = held + lane; i < want; i += 64) take(p, list + i, a.ws.free_pages[next + i - held]);
+    for (int i = held + lane; i < want; i += 64) take(p, list + i, handed_out(next + i - held));
+    for (int i = want + lane; i < held; i += 64) {   // what the list no longer holds
+      release(p, before[i]);
+      list[i] = -1;
+    }
     if (lane == 0) {
+      Move m = a.ws.moves[s];
       if (KIND == PLAN_RESERVE) {
         if (!first_replaced) a.ws.moves[s] = {0, 0, 0, 0};
       } else {
         // a page of its own in front: the rows that stay where they are come with it
         if (first_replaced) a.ws.moves[s].begin = first * p.page_tokens;
-        p.d_length[s] = a.ws.moves[s].end;
+        p.d_length[s] = m.end;
       }
-    }
-  }
-  __syncthreads();
-  // what the lists no longer hold
-  for (int s = wave; s < p.n_seqs; s += PLAN_WAVES) {
-    const int want = s_want[s], held = s_held[s];
-    if (want < 0) continue;
-    int* list = p.d_table + (size_t)s * p.max_pages;
-    const int* before = a.ws.before + (size_t)s * p.max_pages;
-    for (int i = s_first[s] + lane; i < s_last[s]; i += 64) {
-      if (list[i] != before[i]) release(p, before[i]);
-    }
-    for (int i = max(want, 0) + lane; i < held; i += 64) {
-      release(p, before[i]);
-      list[i] = -1;
     }
   }
 }
@@ -302,7 +318,7 @@ __global__ __launch_bounds__(256) void pages_move_kernel(pi0_pages p, PlanSpace 
       data[u] = uint4{};
       if (row < deep && pos < m.end) {
         const int src = pos < m.from ? pos : m.from + keep[pos - m.from];
-        const int to = now[pos >> shift], from = src >= 0 && (src >> shift) < m.held ? before[src >> shift] : -1;
+        const int to = now[pos >> shift], from = src >= 0 && (src >> shift) < m.held ? before[src >> shift] & ~SHARED : -1;
         if ((unsigned)to < (unsigned)p.n_pages && (unsigned)from < (unsigned)p.n_pages) {
           dst[u] = 2 * (to * p.page_stride + (pos & mask) * p.token_stride);
           data[u] = *reinterpret_cast<const uint4*>(pool + 2 * (from * p.page_stride + (src & mask) * p.token_stride));
@@ -332,7 +348,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void pages_fork_kernel(pi0_pages p, c
       continue;
     }
     const int length = p.d_length[s];
-    if (length < 0 || length > pages_held(p, s, lane) * p.page_tokens) s_bad = 1;
+    if (length < 0 || length > pages_held(p, s, lane, page_at(p, s, lane)) * p.page_tokens) s_bad = 1;
     if (lane == 0) atomicOr(&s_mark[s], 1);
   }
   __syncthreads();
@@ -347,7 +363,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void pages_fork_kernel(pi0_pages p, c
   }
   for (int i = wave; i < n; i += PLAN_WAVES) {
     const int s = s_src[i], d = s_dst[i], length = length_of(p, s), shared = div_up(length, p.page_tokens);
-    const int held = pages_held(p, d, lane);
+    const int held = pages_held(p, d, lane, page_at(p, d, lane));
     int* list = p.d_table + (size_t)d * p.max_pages;
     for (int j = lane; j < max(shared, held); j += 64) {
       const int old = j < held ? list[j] : -1, page = j < shared ? page_at(p, s, j) : -1;
