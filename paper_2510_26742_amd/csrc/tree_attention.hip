@@ -44,43 +44,33 @@ struct Mat<f16> {
   }
 };
 
-// How the work is cut.  A unit is a tile of 16 R RW rows of one sequence and key/value head against all of its keys, in granules of 32
+// How the work is cut.  A unit is a tile of 64 R rows of one sequence and key/value head against all of its keys, in granules of 32
 // keys.  Lengths differ, and the host does not know them, so every block works out from the lengths which granules are its
-// own: the units lie behind each other on a line that is cut into runs of equal length, one per block.
-//   - Few units (at most half as many as blocks): each takes up a whole number of runs, so that a block has part of one unit
-//     only; the shortest run, in steps of an eighth, for which there are blocks enough.  The row tiles of a head lie side by side, part
-//     by part, and neighbouring runs go to blocks of one die: its L2 gives the same keys to all of them.
-//   - Many: the line is dense, except that a unit is START granules longer than it is - what a block spends before a unit's
-//     first granule and behind its last -, and a run may end one unit, hold others and begin the next.
-// A block writes a unit that it has all of; of any other it leaves a partial result, in slot 1 if it has the first granule, in slot 0
-// if not, and the second launch joins them.
-constexpr int GRANULE = 32, START = 6;
+// own: the units lie behind each other on a line that is cut into runs of equal length, one per block.  A unit is START granules longer
+// than it is - what a block spends before a unit's first granule and behind its last -, and a run, LEAST long at least, may end one
+// unit, hold others and begin the next.  A block writes a unit that it has all of; of any other it leaves a partial result, in slot 1 if it
+// has the first granule, in slot 0 if not, and the second launch joins them.
+// LEAST: of few keys, 1 or 2 make more partial results than their reading at once is worth (4 x 8 tokens over up to 4096, 8 heads over 1 of
+// 256: 19.6 us with 1, 15.2 with 2, 14.1 with 3), many take longer one behind the other (1 token over 816: 8.7, 9.5, 9.4, with 4 10.9).
+// START from 2 to 12 changes nothing by more than 1 %, except that 2 lets row tiles of the same keys drift apart (8 x 64 over 16384 in tiles of 64
+// rows: 75.8 us with 2, 61.9 with 6).
+constexpr int GRANULE = 32, START = 6, LEAST = 3;
 
-// A stage of K and V tiles is 128 D bytes; STAGES of them per block.  Few rows: what counts is bytes in flight and, beside them,
-// other blocks that read while one begins or ends a unit, so blocks are small and several share a compute unit.  BLOCKS: as
-// many as the chip's 256 hold at once.
-template <int D, int RW, int R>
+// A stage of K and V tiles is 128 D bytes; STAGES of them per block.  BLOCKS: as many as the chip's 256 compute units hold at once, two
+// or more to each where registers let them: one reads while another begins or ends a unit.
+// Blocks of 1 or 2 waves for few rows are no faster than those of 4 with a wave or two that only request (64 x 1 over up to 8192:
+// 53.3, 52.0, 51.5 us; 1 over 816: 9.8, 9.0, 8.7).
+template <int D, int R>
 struct Shape;
-template <> struct Shape<256, 1, 1> { static constexpr int STAGES = 2, BLOCKS = 512; };
-template <> struct Shape<256, 2, 1> { static constexpr int STAGES = 2, BLOCKS = 512; };
-template <> struct Shape<256, 4, 1> { static constexpr int STAGES = 2, BLOCKS = 512; };
-template <> struct Shape<256, 4, 2> { static constexpr int STAGES = 4, BLOCKS = 256; };
-template <> struct Shape<128, 1, 1> { static constexpr int STAGES = 2, BLOCKS = 1024; };
-template <> struct Shape<128, 2, 1> { static constexpr int STAGES = 4, BLOCKS = 512; };
-template <> struct Shape<128, 4, 1> { static constexpr int STAGES = 4, BLOCKS = 512; };
-template <> struct Shape<128, 4, 2> { static constexpr int STAGES = 4, BLOCKS = 512; };
-template <> struct Shape<64, 1, 1> { static constexpr int STAGES = 4, BLOCKS = 1024; };
-template <> struct Shape<64, 2, 1> { static constexpr int STAGES = 4, BLOCKS = 1024; };
-template <> struct Shape<64, 4, 1> { static constexpr int STAGES = 4, BLOCKS = 512; };
-template <> struct Shape<64, 4, 2> { static constexpr int STAGES = 4, BLOCKS = 512; };
+template <> struct Shape<256, 1> { static constexpr int STAGES = 2, BLOCKS = 512; };
+template <> struct Shape<256, 2> { static constexpr int STAGES = 4, BLOCKS = 256; };
+template <> struct Shape<128, 1> { static constexpr int STAGES = 4, BLOCKS = 512; };
+template <> struct Shape<128, 2> { static constexpr int STAGES = 4, BLOCKS = 512; };
+template <> struct Shape<64, 1> { static constexpr int STAGES = 4, BLOCKS = 512; };
+template <> struct Shape<64, 2> { static constexpr int STAGES = 4, BLOCKS = 512; };
 
-// Where a unit lies on the line.  length: of the unit's share of the line, front: how far behind its beginning the first granule is
-struct Cut {
-  int run;
-  int whole;   // units take up whole runs
-  __device__ __forceinline__ int parts(int granules) const { return (int)((unsigned)(granules + run - 1) / (unsigned)run); }
-  __device__ __forceinline__ int length(int granules) const { return whole ? parts(granules) * run : granules > 0 ? granules + START : 0; }
-};
+// a unit's share of the line
+__device__ __forceinline__ int share_of(int granules) { return granules > 0 ? granules + START : 0; }
 
 struct TreeArgs {
   pi0_pages p;
@@ -98,7 +88,7 @@ struct TreeArgs {
   int64_t layer;         // elements in front of the layer
   // workspace
   int* upto;             // [n_seqs] where a sequence's share of the line ends
-  Cut* cut;
+  int* run;              // granules per run
   f32x4* part_o;         // [runs][2][rows of a tile / 16][head_dim / 16][64]: as a wave holds them
   float2* part_ml;       // [runs][2][rows of a tile]: reference of the exponents, sum of the weights
 };
@@ -187,78 +177,52 @@ __device__ __forceinline__ int wave_prefix(int v) {   // sum over the lanes up t
   return v;
 }
 
-// RW waves of a block have R times 16 rows each and read the same tiles
-template <class T, int D, int RW, int R>
-__global__ __launch_bounds__(64 * RW, RW >= 4 && (D < 256 || R == 1) ? 2 : 1) void tree_attention_kernel(TreeArgs a) {
-  constexpr int STAGES = Shape<D, RW, R>::STAGES, BLOCKS = Shape<D, RW, R>::BLOCKS, ROWS = 16 * R * RW;
+// 4 waves of a block have R times 16 rows each and read the same tiles
+constexpr int RW = 4;
+template <class T, int D, int R>
+__global__ __launch_bounds__(64 * RW, D < 256 || R == 1 ? 2 : 1) void tree_attention_kernel(TreeArgs a) {
+  constexpr int STAGES = Shape<D, R>::STAGES, BLOCKS = Shape<D, R>::BLOCKS, ROWS = 16 * R * RW;
   constexpr int PIECES = D / 8, TILE = 32 * D * 2, PARTS = TILE / 1024, REQUESTS = 2 * PARTS / RW, KEYS_PER_REQUEST = 512 / D;
   constexpr int AHEAD = R > 1;
   constexpr int STEPS = D / 32, TILES = D / 16;   // of 32 d that scores are summed over, of 16 d that sums are kept for
-  static_assert(REQUESTS >= 1 && STAGES >= (AHEAD ? 3 : 2) && (!AHEAD || RW == 4) && (STAGES - 2) * REQUESTS < 64, "the wait counter holds what is in flight");
+  static_assert(REQUESTS >= 1 && STAGES >= (AHEAD ? 3 : 2) && (STAGES - 2) * REQUESTS < 64, "the wait counter holds what is in flight");
   typedef T T2 __attribute__((ext_vector_type(2)));
   typedef T T4 __attribute__((ext_vector_type(4)));
   const pi0_pages& p = a.p;
   __shared__ __align__(1024) unsigned char tiles[STAGES][2][TILE];
-  __shared__ int2 line_of[MAX_SEQS];   // units and granules of a sequence, then where its share of the line ends (x)
+  __shared__ int end_of[MAX_SEQS];   // where a sequence's share of the line ends
   const int lane = threadIdx.x & 63, rw = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), quad = lane >> 4;
 
   // The line, worked out by every wave for itself: lane l has the sequences l, l + 64, ..; what it knows of the first 64 stays in
   // registers.  (Whatever runs once per block is written to be short: a block starts with its code far away, and 64 bytes
   // of it cost about as long as a read of memory that is near.)
-  Cut cut;
-  int line, my_end = 0;
-  int2 my_rows = {0, 0}, mine = {0, 0};
+  int line, my_end = 0, run;
+  int2 my_rows = {0, 0};
   int my_length = 0;
   {
-    float units = 0.f, total = 0.f;
-#pragma unroll 1
-    for (int s = lane; s < p.n_seqs; s += 64) {
-      const int2 rows = rows_of(a.row_start, s, a.n_rows, a.max_rows);
-      const int length = length_of(p, s);
-      const int2 here = {p.kv_heads * div_up(rows.y * a.group, ROWS), div_up(min(length + rows.y, p.max_pages * p.page_tokens), GRANULE)};
-      if (s == lane) my_rows = rows, my_length = length, mine = here;
-      else line_of[s] = here;   // (each wave the same, and a lane reads only what it has written itself)
-      units += (float)here.x;
-      total += (float)here.x * (float)here.y;
-    }
-    units = wave_sum(units), total = wave_sum(total);
-    cut.whole = units <= BLOCKS / 2;
-    cut.run = max(1, (int)ceilf(total * (1.f / BLOCKS)));
-    if (cut.whole) {
-      // (sums of whole numbers that matter only up to BLOCKS: exact where they decide.  Ends with one part per unit at the latest)
-      const int more = cut.run / 8 + 1;
-#pragma unroll 1
-      for (;; cut.run += more) {
-        float blocks = 0.f;
-#pragma unroll 1
-        for (int s = lane; s < p.n_seqs; s += 64) {
-          const int2 here = s == lane ? mine : line_of[s];
-          blocks += (float)here.x * (float)cut.parts(here.y);
-        }
-        if (wave_sum(blocks) <= BLOCKS) break;
-      }
-    }
     int before = 0;
 #pragma unroll 1
     for (int s0 = 0; s0 < p.n_seqs; s0 += 64) {
       const int s = s0 + lane;
-      const int2 here = s0 == 0 ? mine : s < p.n_seqs ? line_of[s] : int2{0, 0};
-      const int end = before + wave_prefix(here.x * cut.length(here.y));
+      int2 rows = {0, 0};
+      int length = 0;
+      if (s < p.n_seqs) rows = rows_of(a.row_start, s, a.n_rows, a.max_rows), length = length_of(p, s);
+      const int units = p.kv_heads * div_up(rows.y * a.group, ROWS), granules = div_up(min(length + rows.y, p.max_pages * p.page_tokens), GRANULE);
+      const int end = before + wave_prefix(units * share_of(granules));
+      if (s0 == 0) my_rows = rows, my_length = length;
       if (s0 == 0) my_end = end;
       if (rw == 0 && s < p.n_seqs) {
-        line_of[s].x = end;
+        end_of[s] = end;
         if (blockIdx.x == 0) a.upto[s] = end;
       }
       before = __builtin_amdgcn_readlane(end, 63);
     }
     line = before;
-    if (!cut.whole) cut.run = max(1, div_up(line, BLOCKS));
-    if (blockIdx.x == 0 && threadIdx.x == 0) *a.cut = cut;
+    run = max(LEAST, div_up(line, BLOCKS));
+    if (blockIdx.x == 0 && threadIdx.x == 0) *a.run = run;
     if (p.n_seqs > 64) __syncthreads();
   }
-  // blocks go to the chip's eight dies in turn
-  const int mine_run = (blockIdx.x & 7) * (BLOCKS / 8) + (blockIdx.x >> 3);
-  const int begin = (int)min((int64_t)line, (int64_t)mine_run * cut.run), end = (int)min((int64_t)line, (int64_t)begin + cut.run);
+  const int begin = (int)min((int64_t)line, (int64_t)blockIdx.x * run), end = (int)min((int64_t)line, (int64_t)begin + run);
 
   // This lane's pieces.  First product: keys lane % 16 and that + 16, pieces quad, quad + 4, ..; second: of 4 keys and 16 d that 16
   // lanes read transposed, key (lane % 16) / 4 and 4 d of lane % 4.  Requests: row lane / PIECES of a KiB, its piece lane % PIECES -
@@ -284,31 +248,22 @@ __global__ __launch_bounds__(64 * RW, RW >= 4 && (D < 256 || R == 1) ? 2 : 1) vo
     } else {
       for (int top = p.n_seqs - 1; seq < top;) {
         const int mid = (seq + top) >> 1;
-        if (line_of[mid].x <= cur) seq = mid + 1;
+        if (end_of[mid] <= cur) seq = mid + 1;
         else top = mid;
       }
       seq = uniform(seq);
-      before = uniform(seq > 0 ? line_of[seq - 1].x : 0);
+      before = uniform(seq > 0 ? end_of[seq - 1] : 0);
       rows = rows_of(a.row_start, seq, a.n_rows, a.max_rows);
       rows.x = uniform(rows.x), rows.y = uniform(rows.y);
       length = uniform(length_of(p, seq));
     }
     const int total = min(length + rows.y, p.max_pages * p.page_tokens), granules = div_up(total, GRANULE), row_tiles = div_up(rows.y * a.group, ROWS);
-    const int inside = cur - before, room = cut.length(granules) * row_tiles;   // of a key/value head
+    const int share = granules + START, inside = cur - before, room = share * row_tiles;   // of a key/value head
     const int kv_head = p.kv_heads > 1 ? (unsigned)inside / (unsigned)room : 0, in_head = inside - kv_head * room;
-    int row_tile, g0, g1;
-    if (cut.whole) {
-      const int chunk = (unsigned)in_head / (unsigned)cut.run, part = row_tiles > 1 ? (unsigned)chunk / (unsigned)row_tiles : chunk;
-      row_tile = chunk - part * row_tiles;
-      g0 = part * cut.run, g1 = min(granules, g0 + cut.run);
-      cur = end;
-    } else {
-      row_tile = row_tiles > 1 ? (unsigned)in_head / (unsigned)(granules + START) : 0;
-      const int first = before + kv_head * room + row_tile * (granules + START) + START;
-      g0 = max(0, cur - first), g1 = min(granules, end - first);
-      cur = first + granules;
-      if (g0 >= g1) continue;   // the run ends in front of the unit's first granule
-    }
+    const int row_tile = row_tiles > 1 ? (unsigned)in_head / (unsigned)share : 0;
+    const int first = before + kv_head * room + row_tile * share + START, g0 = max(0, cur - first), g1 = min(granules, end - first);
+    cur = first + granules;
+    if (g0 >= g1) continue;   // the run ends in front of the unit's first granule
 
     // The pages of the first granules.  With AHEAD the last granule is requested again where there is none behind it, into a stage that
     // nobody reads any more: as many requests are on their way at the end as anywhere, and no branch parts the products.
@@ -351,18 +306,19 @@ __global__ __launch_bounds__(64 * RW, RW >= 4 && (D < 256 || R == 1) ? 2 : 1) vo
 
     // Requests of this wave's part of a granule, of whose keys the first and last 16 lie in pages page0 and page1.  Where there is no page
     // (-1), and behind the last position, some row is read that the scores then hide.  A quarter of a granule is 16 keys, or the
-    // values of 16; a wave has one, two or all four.
+    // values of 16: one for each wave.
     constexpr int QUARTER = PARTS / 2;   // KiB
+    const bool of_v = rw >= 2;
     struct Quarter {
       const char* from;
       unsigned to;
     };
-    auto quarter_of = [&](int quarter, int granule, int stage, int page0, int page1) {
-      const int pos = granule * GRANULE + (quarter & 1) * 16, page = max(quarter & 1 ? page1 : page0, 0);
+    auto quarter_of = [&](int granule, int stage, int page0, int page1) {
+      const int pos = granule * GRANULE + (rw & 1) * 16, page = max(rw & 1 ? page1 : page0, 0);
       const uint64_t in = (uint64_t)(unsigned)(pos & in_page) * (unsigned)p.token_stride;
-      return Quarter{(quarter >= 2 ? pool_v : pool_k) + 2 * (page * p.page_stride + in), lds0 + stage * 2 * TILE + quarter * QUARTER * 1024};
+      return Quarter{(of_v ? pool_v : pool_k) + 2 * (page * p.page_stride + in), lds0 + stage * 2 * TILE + rw * QUARTER * 1024};
     };
-    auto request_kib = [&](const Quarter& at, bool of_v, int kib) {
+    auto request_kib = [&](const Quarter& at, int kib) {
       // how far the first key's number turns the pieces of its row (the rest is in piece0)
       const int key = kib * KEYS_PER_REQUEST, turn_k = D == 64 ? key >> 1 & 7 : key, turn_v = D == 64 ? 0 : (key & 7) << 1;
       // (15 strides and a row fit 32 bits)
@@ -370,12 +326,9 @@ __global__ __launch_bounds__(64 * RW, RW >= 4 && (D < 256 || R == 1) ? 2 : 1) vo
       asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(at.to), "v"(off), "s"(at.from), "n"(kib * 1024) : "memory", "scc");
     };
     auto request = [&](int granule, int stage, int page0, int page1) {
-#pragma unroll 1
-      for (int quarter = rw; quarter < 4; quarter += RW) {
-        const Quarter at = quarter_of(quarter, granule, stage, page0, page1);
+      const Quarter at = quarter_of(granule, stage, page0, page1);
 #pragma unroll
-        for (int kib = 0; kib < QUARTER; kib++) request_kib(at, quarter >= 2, kib);
-      }
+      for (int kib = 0; kib < QUARTER; kib++) request_kib(at, kib);
     };
 
     RowState<D> st[R];
@@ -414,7 +367,7 @@ __global__ __launch_bounds__(64 * RW, RW >= 4 && (D < 256 || R == 1) ? 2 : 1) vo
       unsigned char* const at = tiles[stage][1] + lane * 16;
       bool odd = false;
       for (int part = rw; part < PARTS; part += RW) odd |= clean<T, false>(at + part * 1024);
-      if (RW > 1 ? __syncthreads_or(odd) : __ballot(odd) != 0) {
+      if (__syncthreads_or(odd)) {
         odd_from = min(odd_from, granule);
         for (int part = rw; part < PARTS; part += RW) (void)clean<T, true>(at + part * 1024);
         __syncthreads();
@@ -555,7 +508,7 @@ __global__ __launch_bounds__(64 * RW, RW >= 4 && (D < 256 || R == 1) ? 2 : 1) vo
     };
 
     int stage = 0;
-    if (RW > 1 && row_tile * ROWS + rw * R * 16 >= rows.y * a.group) {
+    if (row_tile * ROWS + rw * R * 16 >= rows.y * a.group) {
       // a wave without rows: its part of the requests, and what all waves do together
       if (AHEAD) arrived(g0, std::integral_constant<int, STAGES - 2>());
 #pragma unroll 1
@@ -583,11 +536,11 @@ __global__ __launch_bounds__(64 * RW, RW >= 4 && (D < 256 || R == 1) ? 2 : 1) vo
         clean_values(granule, stage, none >> (2 * (STAGES - 2)) & 3);
         const int stage1 = stage + 1 == STAGES ? 0 : stage + 1, wanted = granule + STAGES - 1;
         next_pages();
-        const Quarter at = quarter_of(rw, in_unit(wanted), stage == 0 ? STAGES - 1 : stage - 1, page0, page1);
+        const Quarter at = quarter_of(in_unit(wanted), stage == 0 ? STAGES - 1 : stage - 1, page0, page1);
         scores(stage1, s_next, [&](int i) {
           first_values(stage, i);
 #pragma unroll
-          for (int j = i * QUARTER / STEPS; j < (i + 1) * QUARTER / STEPS; j++) request_kib(at, rw >= 2, j);
+          for (int j = i * QUARTER / STEPS; j < (i + 1) * QUARTER / STEPS; j++) request_kib(at, j);
 #pragma unroll
           for (int j = i * 4 * R / STEPS; j < (i + 1) * 4 * R / STEPS; j++) weigh(s, j);
         });
@@ -655,7 +608,7 @@ __global__ __launch_bounds__(64 * RW, RW >= 4 && (D < 256 || R == 1) ? 2 : 1) vo
           *reinterpret_cast<T4*>(out + b * 16 + 4 * quad) = w;
         }
       } else {
-        const size_t set = ((size_t)mine_run * 2 + (g0 == 0)) * (ROWS / 16) + rw * R + n;
+        const size_t set = ((size_t)blockIdx.x * 2 + (g0 == 0)) * (ROWS / 16) + rw * R + n;
 #pragma unroll
         for (int b = 0; b < TILES; b++) a.part_o[(set * TILES + b) * 64 + lane] = row.o[b];
         if (quad == 0) a.part_ml[set * 16 + kkey] = make_float2(row.m, row.l);
@@ -666,38 +619,32 @@ __global__ __launch_bounds__(64 * RW, RW >= 4 && (D < 256 || R == 1) ? 2 : 1) vo
 
 // The rows of units that several blocks had a part in: sum_z 2^(m_z - m) o_z / sum_z 2^(m_z - m) l_z, in the order of the keys.  A wave
 // has 16 d of 16 rows, as the partial results lie; WPR waves share out the parts: 8 where units are so few that each has many.
-template <class T, int D, int RW, int R, int WPR>
+template <class T, int D, int R, int WPR>
 __global__ __launch_bounds__(512) void tree_merge_kernel(TreeArgs a) {
   constexpr int ROWS = 16 * R * RW, TILES = D / 16, BATCH = 4;
   typedef T T4 __attribute__((ext_vector_type(4)));
   const pi0_pages& p = a.p;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, share = wave % WPR, kkey = lane & 15, quad = lane >> 4;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, nth = wave % WPR, kkey = lane & 15, quad = lane >> 4;
   const int item = blockIdx.x * (8 / WPR) + wave / WPR, set = item / TILES, tile = item % TILES, kv_head = blockIdx.y, seq = blockIdx.z;
   const int2 rows = rows_of(a.row_start, seq, a.n_rows, a.max_rows);
   if (set * 16 >= rows.y * a.group) return;   // (with WPR == 8 all of a block's waves)
   const int total = min(length_of(p, seq) + rows.y, p.max_pages * p.page_tokens);
   const int granules = div_up(total, GRANULE), row_tiles = div_up(rows.y * a.group, ROWS), row_tile = set / (ROWS / 16);
-  const Cut cut = *a.cut;
-  const int before = (seq > 0 ? a.upto[seq - 1] : 0) + kv_head * row_tiles * cut.length(granules);
-  int run0, parts, step = 1;   // the runs that had a part
-  if (cut.whole) {
-    run0 = before / cut.run + row_tile, parts = cut.parts(granules), step = row_tiles;
-  } else {
-    const int first = before + row_tile * (granules + START) + START;
-    run0 = first / cut.run, parts = (first + granules - 1) / cut.run - run0 + 1;
-  }
+  const int run = *a.run, share = granules + START;
+  const int first = (seq > 0 ? a.upto[seq - 1] : 0) + (kv_head * row_tiles + row_tile) * share + START;
+  const int run0 = first / run, parts = (first + granules - 1) / run - run0 + 1;   // the runs that had a part
   if (parts < 2) return;
   // this wave's parts, each row against the maximum of its own so far; what a row that is not there holds stays in its lanes
   f32x4 o = {};
   float m = -INFINITY, l = 0.f;
 #pragma unroll 1
-  for (int part = share; part < parts; part += BATCH * WPR) {
+  for (int part = nth; part < parts; part += BATCH * WPR) {
     float2 ml[BATCH];
     f32x4 v[BATCH];
 #pragma unroll
     for (int i = 0; i < BATCH; i++) {
       const int z = part + i * WPR;
-      const size_t from = ((size_t)(run0 + min(z, parts - 1) * step) * 2 + (z == 0)) * (ROWS / 16) + set % (ROWS / 16);
+      const size_t from = ((size_t)(run0 + min(z, parts - 1)) * 2 + (z == 0)) * (ROWS / 16) + set % (ROWS / 16);
       ml[i] = a.part_ml[from * 16 + kkey];
       v[i] = a.part_o[(from * TILES + tile) * 64 + lane];
       if (z >= parts) ml[i].x = -INFINITY, v[i] = f32x4{};
@@ -716,10 +663,10 @@ __global__ __launch_bounds__(512) void tree_merge_kernel(TreeArgs a) {
   if constexpr (WPR > 1) {
     __shared__ float2 s_ml[WPR][16];
     __shared__ f32x4 s_o[WPR][64];
-    if (quad == 0) s_ml[share][kkey] = make_float2(m, l);
-    s_o[share][lane] = o;
+    if (quad == 0) s_ml[nth][kkey] = make_float2(m, l);
+    s_o[nth][lane] = o;
     __syncthreads();
-    if (share != 0) return;
+    if (nth != 0) return;
     for (int w = 1; w < WPR; w++) m = fmaxf(m, s_ml[w][kkey].x);
     o = f32x4{}, l = 0.f;
     for (int w = 0; w < WPR; w++) {
@@ -739,31 +686,26 @@ __global__ __launch_bounds__(512) void tree_merge_kernel(TreeArgs a) {
 }
 
 struct Space {
-  size_t part_ml, upto, cut, bytes;   // part_o lies in front
+  size_t part_ml, upto, run, bytes;   // part_o lies in front
 };
-template <int D, int RW, int R>
+template <int D, int R>
 Space space_of(const pi0_pages& p) {
   Space s;
-  const size_t slots = (size_t)Shape<D, RW, R>::BLOCKS * 2 * 16 * R * RW;
+  const size_t slots = (size_t)Shape<D, R>::BLOCKS * 2 * 16 * R * RW;
   s.part_ml = slots * D * sizeof(float);
   s.upto = s.part_ml + slots * sizeof(float2);
-  s.cut = s.upto + (size_t)p.n_seqs * sizeof(int);
-  s.bytes = s.cut + sizeof(Cut);
+  s.run = s.upto + (size_t)p.n_seqs * sizeof(int);
+  s.bytes = s.run + sizeof(int);
   return s;
 }
 
-// f<RW, R>(): 16, 32, 64 or 128 rows per tile, the least that all rows of a sequence and key/value head fit - its keys are read once
-// then -, and as many as the registers hold where they are more.
-template <int D, class F>
-auto with_rows(int rows, F f) {
-  using std::integral_constant;
-  constexpr integral_constant<int, 1> one;
-  constexpr integral_constant<int, 2> two;
-  constexpr integral_constant<int, 4> four;
-  if (rows <= 16) return f(one, one);
-  if (rows <= 32) return f(two, one);
-  if (rows <= 64) return f(four, one);
-  return f(four, two);
+// f(R): 64 rows per tile, or 128 where there are more than that of enough sequences and heads (measured with 64 and with 128: 8 x 64 nodes
+// with 8 heads over 1 of 256 and 16384 keys 61.8 and 57.3 us, 16 x 33 with 32 over 8 of 128 and 4096 51.5 and 44.8; 1 x 64 over 2048
+// 20.8 and 23.4, 16 x 16, that is 128 rows, over 2048 20.2 and 23.3).
+template <class F>
+auto with_rows(int rows, int heads, F f) {
+  if (rows > 128 && heads >= 4) return f(std::integral_constant<int, 2>());
+  return f(std::integral_constant<int, 1>());
 }
 template <class F>
 auto with_dim(int head_dim, F f) {
@@ -774,7 +716,7 @@ auto with_dim(int head_dim, F f) {
 
 Space space_of(const pi0_pages& p, int heads, int max_rows) {
   return with_dim(p.head_dim, [&](auto d) {
-    return with_rows<d>(max_rows * (heads / p.kv_heads), [&](auto rw, auto r) { return space_of<d, rw, r>(p); });
+    return with_rows(max_rows * (heads / p.kv_heads), p.n_seqs * p.kv_heads, [&](auto r) { return space_of<d, r>(p); });
   });
 }
 
@@ -782,20 +724,20 @@ template <class T>
 void launch(hipStream_t s, TreeArgs& a, char* ws) {
   with_dim(a.p.head_dim, [&](auto d) {
     const int rows = a.max_rows * a.group;
-    with_rows<d>(rows, [&](auto rw, auto r) {
-      constexpr int D = d, RW = rw, R = r, BLOCKS = Shape<D, RW, R>::BLOCKS;
-      const Space at = space_of<D, RW, R>(a.p);
+    with_rows(rows, a.p.n_seqs * a.p.kv_heads, [&](auto r) {
+      constexpr int D = d, R = r, BLOCKS = Shape<D, R>::BLOCKS;
+      const Space at = space_of<D, R>(a.p);
       a.part_o = reinterpret_cast<f32x4*>(ws);
       a.part_ml = reinterpret_cast<float2*>(ws + at.part_ml);
       a.upto = reinterpret_cast<int*>(ws + at.upto);
-      a.cut = reinterpret_cast<Cut*>(ws + at.cut);
-      hipLaunchKernelGGL((tree_attention_kernel<T, D, RW, R>), dim3(BLOCKS), dim3(64 * RW), 0, s, a);
+      a.run = reinterpret_cast<int*>(ws + at.run);
+      hipLaunchKernelGGL((tree_attention_kernel<T, D, R>), dim3(BLOCKS), dim3(64 * RW), 0, s, a);
       const int units = a.p.n_seqs * a.p.kv_heads * div_up(rows, 16 * R * RW);
       const int items = div_up(rows, 16) * (D / 16);   // of 16 rows and 16 d
       if (units <= BLOCKS / 16)
-        hipLaunchKernelGGL((tree_merge_kernel<T, D, RW, R, 8>), dim3(items, a.p.kv_heads, a.p.n_seqs), dim3(512), 0, s, a);
+        hipLaunchKernelGGL((tree_merge_kernel<T, D, R, 8>), dim3(items, a.p.kv_heads, a.p.n_seqs), dim3(512), 0, s, a);
       else
-        hipLaunchKernelGGL((tree_merge_kernel<T, D, RW, R, 1>), dim3(div_up(items, 8), a.p.kv_heads, a.p.n_seqs), dim3(512), 0, s, a);
+        hipLaunchKernelGGL((tree_merge_kernel<T, D, R, 1>), dim3(div_up(items, 8), a.p.kv_heads, a.p.n_seqs), dim3(512), 0, s, a);
       return 0;
     });
     return 0;
