@@ -7,10 +7,10 @@
 // are counted as they lie there: probabilities go from one product into the next without leaving their lane, row sums and
 // maxima need two exchanges between the quarters of a wave.  V^T is read out of row-major tiles with the transposing LDS
 // load (4 keys x 16 d per 16 lanes).  A wave has R times 16 rows: what it reads of K and V out of LDS serves all of them.  R = 1 where
-// the cache's own bytes are what the time goes to (up to 64 rows), 2 where there are more.
-// What bounds it: few rows the reads of the cache (64 x 1 token, 8 heads over 1 of 256, up to 8192 keys: 277 MB in 50 us, 5.5 TB/s);
-// many rows the issue of instructions, of which a wave that is alone on its SIMD has one per 4 cycles (8 x 64 nodes over 16384: 470
-// TFLOP/s; a granule's 64 products per wave could end in 1024 cycles and take 1900), which is why the loop does nothing that
+// the cache's own bytes are what the time goes to, 2 where rows are many.
+// What bounds it: few rows the reads of the cache (64 x 1 token, 8 heads over 1 of 256, up to 8192 keys: 277 MB in 43 us, 6.4 TB/s);
+// many rows the issue of instructions, of which a wave that is alone on its SIMD has one per 4 cycles (8 x 64 nodes over 16384: 25.7
+// GFLOP in 50 us, 510 TFLOP/s; a granule's 64 products per wave could end in 1024 cycles and take 1700), which is why the loop does nothing that
 // can be done in front of it.
 // Tiles come straight into LDS, 16 bytes per lane; the pieces of a row are permuted by its key (on the global side: a lane
 // may fetch any piece) so that neither product's reads collide in the banks.
@@ -52,21 +52,24 @@ struct Mat<f16> {
 // has the first granule, in slot 0 if not, and the second launch joins them.
 // LEAST: of few keys, 1 or 2 make more partial results than their reading at once is worth (4 x 8 tokens over up to 4096, 8 heads over 1 of
 // 256: 19.6 us with 1, 15.2 with 2, 14.1 with 3), many take longer one behind the other (1 token over 816: 8.7, 9.5, 9.4, with 4 10.9).
-// START from 2 to 12 changes nothing by more than 1 %, except that 2 lets row tiles of the same keys drift apart (8 x 64 over 16384 in tiles of 64
-// rows: 75.8 us with 2, 61.9 with 6).
+// START: 12 costs short units up to 4 %, 2 lets row tiles of the same keys drift apart, so that each fetches them for itself (8 x 64 over
+// 16384 in tiles of 64 rows: 75.8 us with 2, 61.9 with 6).
 constexpr int GRANULE = 32, START = 6, LEAST = 3;
 
 // A stage of K and V tiles is 128 D bytes; STAGES of them per block.  BLOCKS: as many as the chip's 256 compute units hold at once, two
-// or more to each where registers let them: one reads while another begins or ends a unit.
-// Blocks of 1 or 2 waves for few rows are no faster than those of 4 with a wave or two that only request (64 x 1 over up to 8192:
-// 53.3, 52.0, 51.5 us; 1 over 816: 9.8, 9.0, 8.7).
+// to each where registers let them: one reads while another begins or ends a unit or waits for its waves.  Heads of 64 have so little
+// work per granule that four pay (64 x 1 over up to 4096, 8 heads over 8: 78.6 us with two, 59.3 with three, 53.0 with four, 79.0 with
+// two of 8 stages; the most that it costs is 4 x 16 over 16384, 8 over 1: 15.7, 16.7, 18.4); those of 128 are as fast with three
+// of 3 stages as with two of 4 (117 us).
+// Blocks of 1 or 2 waves for few rows are no faster than those of 4 with a wave or two that only request (64 x 1 over up to 8192, 8
+// heads over 1 of 256: 53.3, 52.0, 51.5 us; 1 over 816: 9.8, 9.0, 8.7).
 template <int D, int R>
 struct Shape;
 template <> struct Shape<256, 1> { static constexpr int STAGES = 2, BLOCKS = 512; };
 template <> struct Shape<256, 2> { static constexpr int STAGES = 4, BLOCKS = 256; };
 template <> struct Shape<128, 1> { static constexpr int STAGES = 4, BLOCKS = 512; };
 template <> struct Shape<128, 2> { static constexpr int STAGES = 4, BLOCKS = 512; };
-template <> struct Shape<64, 1> { static constexpr int STAGES = 4, BLOCKS = 512; };
+template <> struct Shape<64, 1> { static constexpr int STAGES = 4, BLOCKS = 1024; };
 template <> struct Shape<64, 2> { static constexpr int STAGES = 4, BLOCKS = 512; };
 
 // a unit's share of the line
@@ -618,7 +621,9 @@ __global__ __launch_bounds__(64 * RW, D < 256 || R == 1 ? 2 : 1) void tree_atten
 }
 
 // The rows of units that several blocks had a part in: sum_z 2^(m_z - m) o_z / sum_z 2^(m_z - m) l_z, in the order of the keys.  A wave
-// has 16 d of 16 rows, as the partial results lie; WPR waves share out the parts: 8 where units are so few that each has many.
+// has 16 d of 16 rows, as the partial results lie; WPR waves share out the parts: 8 where units are so few that each has many, with both
+// launches 8 and 1 of 1 token over 16384 12.2 and 30.2 us, of 4 x 8 over 4096 13.9 and 18.0, of 16 x 33 over 4096 51.2 and 44.6.  Bound
+// by the partial results, 64 KiB R per block of heads of 256 and twice that where a run ends one unit and begins another.
 template <class T, int D, int R, int WPR>
 __global__ __launch_bounds__(512) void tree_merge_kernel(TreeArgs a) {
   constexpr int ROWS = 16 * R * RW, TILES = D / 16, BATCH = 4;
