@@ -92,8 +92,9 @@ struct TreeArgs {
   // workspace
   int* upto;             // [n_seqs] where a sequence's share of the line ends
   int* run;              // granules per run
-  f32x4* part_o;         // [runs][2][rows of a tile / 16][head_dim / 16][64]: as a wave holds them
-  float2* part_ml;       // [runs][2][rows of a tile]: reference of the exponents, sum of the weights
+  f32x4* part_o;         // [runs][2][sets][head_dim / 16][64]: as a wave holds them
+  float2* part_ml;       // [runs][2][sets][16]: reference of the exponents, sum of the weights
+  int sets;              // of 16 rows in a tile, or in all there are
 };
 
 // A sequence's entry idx, the same for the whole wave: through the scalar cache, so that it does not wait in line behind the tiles
@@ -611,7 +612,7 @@ __global__ __launch_bounds__(64 * RW, D < 256 || R == 1 ? 2 : 1) void tree_atten
           *reinterpret_cast<T4*>(out + b * 16 + 4 * quad) = w;
         }
       } else {
-        const size_t set = ((size_t)blockIdx.x * 2 + (g0 == 0)) * (ROWS / 16) + rw * R + n;
+        const size_t set = ((size_t)blockIdx.x * 2 + (g0 == 0)) * a.sets + rw * R + n;
 #pragma unroll
         for (int b = 0; b < TILES; b++) a.part_o[(set * TILES + b) * 64 + lane] = row.o[b];
         if (quad == 0) a.part_ml[set * 16 + kkey] = make_float2(row.m, row.l);
@@ -649,7 +650,7 @@ __global__ __launch_bounds__(512) void tree_merge_kernel(TreeArgs a) {
 #pragma unroll
     for (int i = 0; i < BATCH; i++) {
       const int z = part + i * WPR;
-      const size_t from = ((size_t)(run0 + min(z, parts - 1)) * 2 + (z == 0)) * (ROWS / 16) + set % (ROWS / 16);
+      const size_t from = ((size_t)(run0 + min(z, parts - 1)) * 2 + (z == 0)) * a.sets + set % (ROWS / 16);
       ml[i] = a.part_ml[from * 16 + kkey];
       v[i] = a.part_o[(from * TILES + tile) * 64 + lane];
       if (z >= parts) ml[i].x = -INFINITY, v[i] = f32x4{};
@@ -691,12 +692,14 @@ __global__ __launch_bounds__(512) void tree_merge_kernel(TreeArgs a) {
 }
 
 struct Space {
+  int sets;
   size_t part_ml, upto, run, bytes;   // part_o lies in front
 };
 template <int D, int R>
-Space space_of(const pi0_pages& p) {
+Space space_of(const pi0_pages& p, int rows) {
   Space s;
-  const size_t slots = (size_t)Shape<D, R>::BLOCKS * 2 * 16 * R * RW;
+  s.sets = min(4 * R, div_up(rows, 16));
+  const size_t slots = (size_t)Shape<D, R>::BLOCKS * 2 * 16 * s.sets;
   s.part_ml = slots * D * sizeof(float);
   s.upto = s.part_ml + slots * sizeof(float2);
   s.run = s.upto + (size_t)p.n_seqs * sizeof(int);
@@ -720,8 +723,9 @@ auto with_dim(int head_dim, F f) {
 }
 
 Space space_of(const pi0_pages& p, int heads, int max_rows) {
+  const int rows = max_rows * (heads / p.kv_heads);
   return with_dim(p.head_dim, [&](auto d) {
-    return with_rows(max_rows * (heads / p.kv_heads), p.n_seqs * p.kv_heads, [&](auto r) { return space_of<d, r>(p); });
+    return with_rows(rows, p.n_seqs * p.kv_heads, [&](auto r) { return space_of<d, r>(p, rows); });
   });
 }
 
@@ -731,7 +735,8 @@ void launch(hipStream_t s, TreeArgs& a, char* ws) {
     const int rows = a.max_rows * a.group;
     with_rows(rows, a.p.n_seqs * a.p.kv_heads, [&](auto r) {
       constexpr int D = d, R = r, BLOCKS = Shape<D, R>::BLOCKS;
-      const Space at = space_of<D, R>(a.p);
+      const Space at = space_of<D, R>(a.p, rows);
+      a.sets = at.sets;
       a.part_o = reinterpret_cast<f32x4*>(ws);
       a.part_ml = reinterpret_cast<float2*>(ws + at.part_ml);
       a.upto = reinterpret_cast<int*>(ws + at.upto);

@@ -146,6 +146,45 @@ def test_against_the_definition(i):
     c.check()
 
 
+@pytest.mark.parametrize("dtype,d", [("bf16", 256), ("f16", 128), ("bf16", 64)])
+@pytest.mark.parametrize("rows", [15, 16, 17, 63, 64, 65, 127, 128, 129, 200, 257])
+@pytest.mark.parametrize("seqs", [1, 4])
+def test_any_number_of_rows(dtype, d, rows, seqs):
+    """One head per token, so that every number of rows in a tile, and of tiles, occurs; one sequence, and four with fewer and fewer."""
+    print("[gpu] tree_attention", dtype, d, rows, seqs, flush=True)
+    counts = [rows, 1, rows // 2, rows - 1][:seqs]
+    c = Case(rows, [900, 33, 0, 350][:seqs], counts, 1, 1, d, 16, dtype, kind="random")
+    c.run()
+    c.check()
+
+
+@pytest.mark.parametrize("n_seqs", [64, 65, 300, 1024])
+def test_many_sequences(n_seqs):
+    rng = np.random.default_rng(n_seqs)
+    lengths, counts = rng.integers(0, 90, n_seqs).tolist(), rng.integers(0, 3, n_seqs).tolist()
+    lengths[0], lengths[-1], counts[-1] = 2000, 700, 2
+    c = Case(n_seqs, lengths, counts, 4, 2, 64, 32, "f16", kind="tree")
+    c.run()
+    c.check()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("seqs,count", [(1, 3), (4, 20)])
+def test_scores_that_grow_along_the_keys(dtype, seqs, count):
+    """Later keys outweigh all in front of them time and again: what has been summed is scaled down over and over."""
+    c = Case(70, [1500, 700, 64, 3][:seqs], [count] * seqs, 8, 1, 256, 64, dtype, kind="chain")
+    for s in range(seqs):
+        n = c.lengths[s] + count
+        pos = np.arange(n)
+        where = torch.from_numpy(c.table[s][pos // 64]).to(DEV), torch.from_numpy(pos % 64).to(DEV)
+        k = torch.from_numpy(c.k[s]).to(DEV) + 0.02 * torch.arange(n, device=DEV)[:, None, None]
+        c.pages.k[0][where] = k.to(c.dtype)
+        c.k[s] = f64(c.pages.k[0][where])
+    c.q.abs_()
+    c.run()
+    c.check()
+
+
 @pytest.mark.parametrize("spread,scale", [(30.0, None), (1.0, -0.2), (1.0, 0.0), (0.0, None)])
 def test_sharp_negative_and_flat(spread, scale):
     c = Case(50, [300, 70], [5, 40], 8, 1, 256, 32, "bf16", spread=spread)

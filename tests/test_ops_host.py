@@ -127,6 +127,21 @@ def test_tree_attention_refuses(L):
     assert call(size=need - 1) == binding.PI0_ENOMEM
 
 
+def test_strides_and_lines_at_their_limits(L):
+    """Rows 2^27 elements apart, and as many granules of all units together as 2^30, are refused; one step below is taken."""
+    ref = ctypes.byref
+    far = dict(token_stride=1 << 27, page_stride=1 << 34, layer_stride=1 << 38, layers=2, n_pages=2)
+    near = dict(far, token_stride=(1 << 27) - 8)
+    assert L.pi0_tree_attention_workspace_bytes(ref(good(**far)), 8, 1, 1) == 0 and L.pi0_pages_workspace_bytes(ref(good(**far))) == 0
+    assert L.pi0_tree_attention_workspace_bytes(ref(good(**near)), 8, 1, 1) > 0
+    # 1024 sequences, 8 tiles of 16 rows (128 of one key/value head): 2^17 granules and 6 more each are too many, half of that is not
+    wide = dict(n_seqs=1024, page_tokens=256, max_pages=1 << 14, page_stride=256 * 256, layer_stride=10 * 256 * 256)
+    assert L.pi0_tree_attention_workspace_bytes(ref(good(**wide)), 8, 2048, 16) == 0
+    assert L.pi0_tree_attention_workspace_bytes(ref(good(**dict(wide, max_pages=1 << 13))), 8, 2048, 16) > 0
+    # one tile: 2^20 * 1024 positions would pass it too, but a list is shorter than that
+    assert L.pi0_tree_attention_workspace_bytes(ref(good(**dict(wide, max_pages=1 << 16))), 8, 2, 1) > 0
+
+
 def test_store_and_load_refuse(L):
     cfg = synth.reduced_config()
     ctx = ctypes.c_void_p()
