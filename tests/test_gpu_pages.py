@@ -133,6 +133,33 @@ def test_long_compaction_in_place_and_into_own_pages():
         same(gpu, cpu)
 
 
+@pytest.mark.parametrize("first", [0, 63, 511, 512, 1030, 1500])
+def test_lists_and_choices_of_more_than_one_read(first):
+    """119 and more pages, shared by three, of which positions from `first` on close up: shared pages in front of and behind a
+    list's 64th entry are replaced, others not; then a reservation behind them; then a choice with one mistake far behind."""
+    gpu, cpu = make(9, layers=1, n_pages=600, page=16, kv_heads=1, head_dim=64, n_seqs=4, max_pages=150)
+    grow(gpu, cpu, [1900, 0, 0, 40])
+    gpu.pi0_pages_fork(ints([0, 0]), ints([1, 2]))
+    cpu.fork([0, 0], [1, 2])
+    keep = [i for i in range(1900) if i < first or i % 3][:1600]
+    table = np.zeros((4, 1600))
+    table[0, :len(keep)] = keep
+    table[2, :5] = [0, 1, 2, 3, 900]
+    n, start = [len(keep), -1, 5, -1], [0, 1900, 1000, 40]
+    gpu.pi0_pages_compact(ints(table), ints(n), start=ints(start))
+    cpu.compact(table.astype(int), n, start)
+    same(gpu, cpu, "compacted")
+    gpu.pi0_pages_reserve(ints([300, 1, 20, 0]))
+    cpu.reserve([300, 1, 20, 0])
+    same(gpu, cpu, "reserved")
+    table[1, :1600] = np.arange(1600)
+    table[1, 1333] = 1332
+    gpu.pi0_pages_compact(ints(table), ints([-1, 1600, -1, -1]), start=ints([0] * 4))
+    with pytest.raises(binding.Pi0Error):
+        gpu.pi0_pages_status()
+    same(gpu, cpu, "refused")
+
+
 def test_everything_can_be_freed_and_lengths_start_at_nothing():
     gpu, cpu = make(5)
     zero = [0] * 6
