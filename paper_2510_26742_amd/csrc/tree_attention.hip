@@ -10,7 +10,7 @@
 // the cache's own bytes are what the time goes to, 2 where rows are many.
 // What bounds it: few rows the reads of the cache (64 x 1 token, 8 heads over 1 of 256, up to 8192 keys: 277 MB in 43 us, 6.4 TB/s);
 // many rows the issue of instructions, of which a wave that is alone on its SIMD has one per 4 cycles (8 x 64 nodes over 16384: 25.7
-// GFLOP in 50 us, 510 TFLOP/s; a granule's 64 products per wave could end in 1024 cycles and take 1700), which is why the loop does nothing that
+// GFLOP in 49 us, 525 TFLOP/s; a granule's 64 products per wave could end in 1024 cycles, but stand among 350 instructions), which is why the loop does nothing that
 // can be done in front of it.
 // Tiles come straight into LDS, 16 bytes per lane; the pieces of a row are permuted by its key (on the global side: a lane
 // may fetch any piece) so that neither product's reads collide in the banks.
@@ -322,17 +322,29 @@ __global__ __launch_bounds__(64 * RW, D < 256 || R == 1 ? 2 : 1) void tree_atten
       const uint64_t in = (uint64_t)(unsigned)(pos & in_page) * (unsigned)p.token_stride;
       return Quarter{(of_v ? pool_v : pool_k) + 2 * (page * p.page_stride + in), lds0 + stage * 2 * TILE + rw * QUARTER * 1024};
     };
-    auto request_kib = [&](const Quarter& at, int kib) {
-      // how far the first key's number turns the pieces of its row (the rest is in piece0)
-      const int key = kib * KEYS_PER_REQUEST, turn_k = D == 64 ? key >> 1 & 7 : key, turn_v = D == 64 ? 0 : (key & 7) << 1;
-      // (15 strides and a row fit 32 bits)
-      const unsigned off = (my_row + key) * (unsigned)(2 * p.token_stride) + ((of_v ? piece_v0 : piece_k0) ^ (of_v ? turn_v : turn_k)) * 16;
-      asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(at.to), "v"(off), "s"(at.from), "n"(kib * 1024) : "memory", "scc");
+    // 4 KiB (of heads of 64: 2) at once: the instruction's offset counts on both sides, so the LDS address is set once.  (Rows are no
+    // less than a head's bytes apart: what is taken off for it is there.  15 strides and a row fit 32 bits.)
+    constexpr int BURST = QUARTER < 4 ? QUARTER : 4;
+    auto request_burst = [&](const Quarter& at, int burst) {
+      unsigned off[BURST];
+#pragma unroll
+      for (int i = 0; i < BURST; i++) {
+        // how far the first key's number turns the pieces of its row (the rest is in piece0)
+        const int key = (burst * BURST + i) * KEYS_PER_REQUEST, turn_k = D == 64 ? key >> 1 & 7 : key, turn_v = D == 64 ? 0 : (key & 7) << 1;
+        off[i] = (my_row + key) * (unsigned)(2 * p.token_stride) + ((of_v ? piece_v0 : piece_k0) ^ (of_v ? turn_v : turn_k)) * 16 - i * 1024;
+      }
+      if constexpr (BURST == 2)
+        asm volatile("s_add_u32 m0, %0, %4\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %3\n\tglobal_load_lds_dwordx4 %2, %3 offset:1024"
+                     ::"s"(at.to), "v"(off[0]), "v"(off[1]), "s"(at.from), "n"(burst * BURST * 1024) : "memory", "scc");
+      else
+        asm volatile("s_add_u32 m0, %0, %6\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %5\n\tglobal_load_lds_dwordx4 %2, %5 offset:1024\n\t"
+                     "global_load_lds_dwordx4 %3, %5 offset:2048\n\tglobal_load_lds_dwordx4 %4, %5 offset:3072"
+                     ::"s"(at.to), "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(at.from), "n"(burst * BURST * 1024) : "memory", "scc");
     };
     auto request = [&](int granule, int stage, int page0, int page1) {
       const Quarter at = quarter_of(granule, stage, page0, page1);
 #pragma unroll
-      for (int kib = 0; kib < QUARTER; kib++) request_kib(at, kib);
+      for (int burst = 0; burst < QUARTER / BURST; burst++) request_burst(at, burst);
     };
 
     RowState<D> st[R];
@@ -398,7 +410,7 @@ __global__ __launch_bounds__(64 * RW, D < 256 || R == 1 ? 2 : 1) void tree_atten
 #pragma unroll
         for (int n = 0; n < R; n++) {
 #pragma unroll
-          for (int t = 0; t < 2; t++) sum[n][t] = Mat<T>::mfma(kf[i][t], q[n][i], i == 0 ? f32x4{} : sum[n][t]);
+          for (int t = 1; t >= 0; t--) sum[n][t] = Mat<T>::mfma(kf[i][t], q[n][i], i == 0 ? f32x4{} : sum[n][t]);   // (one wait for both)
         }
         beside(i);
         __builtin_amdgcn_sched_barrier(0);
@@ -487,20 +499,30 @@ __global__ __launch_bounds__(64 * RW, D < 256 || R == 1 ? 2 : 1) void tree_atten
 #pragma unroll
       for (int n = 0; n < R; n++) pf[n] = __builtin_bit_cast(s16x8, uint4{pw[n][0], pw[n][1], pw[n][2], pw[n][3]});
 #pragma unroll
-      for (int i = 0; i < TILES; i++) {
-        if (i + LEAD_V < TILES) read_values(stage, i + LEAD_V);
+      for (int i = 0; i < TILES; i += 2) {
 #pragma unroll
-        for (int n = 0; n < R; n++) st[n].o[i] = Mat<T>::mfma(vf[i], pf[n], st[n].o[i]);
+        for (int j = i + LEAD_V; j < i + LEAD_V + 2; j++) {
+          if (j < TILES) read_values(stage, j);
+        }
+#pragma unroll
+        for (int j = i + 1; j >= i; j--) {   // (one wait for both)
+#pragma unroll
+          for (int n = 0; n < R; n++) st[n].o[j] = Mat<T>::mfma(vf[j], pf[n], st[n].o[j]);
+        }
         beside(i);
+        beside(i + 1);
         __builtin_amdgcn_sched_barrier(0);
       }
     };
-    auto maximum = [&](float (&top)[R], const f32x8 (&s)[R], int from, int to) {   // over scores from .. to - 1 of this lane's 8 R
+    // over scores from .. to - 1 of this lane's 8 R, which go from s to `to_s` (and out of the accumulation registers for good)
+    auto maximum = [&](float (&top)[R], f32x8 (&to_s)[R], const f32x8 (&s)[R], int from, int to) {
 #pragma unroll
       for (int i = 0; i < 8 * R; i += 2) {
         if (i < from || i >= to) continue;
-        const float pair = fmaxf(s[i >> 3][i & 7], s[i >> 3][(i & 7) + 1]);
-        top[i >> 3] = (i & 7) == 0 ? pair : fmaxf(top[i >> 3], pair);
+        float a = s[i >> 3][i & 7], b = s[i >> 3][(i & 7) + 1];
+        asm volatile("" : "+v"(a), "+v"(b));
+        to_s[i >> 3][i & 7] = a, to_s[i >> 3][(i & 7) + 1] = b;
+        top[i >> 3] = (i & 7) == 0 ? fmaxf(a, b) : fmaxf(top[i >> 3], fmaxf(a, b));
         asm volatile("" : "+v"(top[i >> 3]));
       }
     };
@@ -532,7 +554,7 @@ __global__ __launch_bounds__(64 * RW, D < 256 || R == 1 ? 2 : 1) void tree_atten
       float top[R];
       scores(0, s, [](int) {});
       hide(s, g0, none >> (2 * (STAGES - 2)) & 3);
-      maximum(top, s, 0, 8 * R);
+      maximum(top, s, s, 0, 8 * R);
       refer_to(top);
 #pragma unroll 1
       for (int granule = g0; granule < g1; granule++) {
@@ -544,16 +566,14 @@ __global__ __launch_bounds__(64 * RW, D < 256 || R == 1 ? 2 : 1) void tree_atten
         scores(stage1, s_next, [&](int i) {
           first_values(stage, i);
 #pragma unroll
-          for (int j = i * QUARTER / STEPS; j < (i + 1) * QUARTER / STEPS; j++) request_kib(at, j);
+          for (int j = i * (QUARTER / BURST) / STEPS; j < (i + 1) * (QUARTER / BURST) / STEPS; j++) request_burst(at, j);
 #pragma unroll
           for (int j = i * 4 * R / STEPS; j < (i + 1) * 4 * R / STEPS; j++) weigh(s, j);
         });
         if (granule + 1 < g1) hide(s_next, granule + 1, none >> (2 * (STAGES - 2)) & 3);
-        sum_values(stage, [&](int i) { maximum(top, s_next, i * 8 * R / TILES, (i + 1) * 8 * R / TILES); });
+        sum_values(stage, [&](int i) { maximum(top, s, s_next, i * 8 * R / TILES, (i + 1) * 8 * R / TILES); });
         next_entries(in_unit(wanted + 1));
         if (granule + 1 < g1) settle(top);
-#pragma unroll
-        for (int n = 0; n < R; n++) s[n] = s_next[n];
         stage = stage1;
       }
     } else {
@@ -567,7 +587,7 @@ __global__ __launch_bounds__(64 * RW, D < 256 || R == 1 ? 2 : 1) void tree_atten
         if (wanted < g1) request(wanted, stage == 0 ? STAGES - 1 : stage - 1, page0, page1);
         scores(stage, s, [&](int i) { first_values(stage, i); });
         hide(s, granule, none >> (2 * (STAGES - 1)) & 3);
-        maximum(top, s, 0, 8 * R);
+        maximum(top, s, s, 0, 8 * R);
         settle(top);
 #pragma unroll
         for (int j = 0; j < 4 * R; j++) weigh(s, j);
