@@ -287,21 +287,23 @@ __global__ __launch_bounds__(PLAN_THREADS) void pages_plan_kernel(PlanArgs a) {
   }
 }
 
-// The rows of a plan.  A block moves one sequence's rows of one layer of the keys or of the values, up to 512 bytes of
-// each: 32 threads of 16 bytes per row, 8 rows side by side, MOVE_ROWS deep.  In place a row only ever moves down, and
+// The rows of a plan.  A block moves 256 bytes of each of one sequence's rows of one layer of the keys or of the values:
+// 16 threads of 16 bytes per row, 16 rows side by side, MOVE_ROWS deep.  In place a row only ever moves down, and
 // ascending sources go to ascending places: the place of a row is no source of a row behind it, so loads may run ahead
 // of stores, and a block-wide wait between the loads of a round and its stores keeps a store from overtaking the load
-// of the row that it replaces.
-constexpr int MOVE_ROWS = 8;
+// of the row that it replaces.  Bound by memory and by the longest sequence's blocks: 32 continuations of 16 prefixes, 6100 rows of 512 bytes
+// of 18 layers, 225 MB, in 85 us with the two plans and the fork around it; with 512 bytes per block and 8 rows deep 105, with 8 rows of
+// 256 bytes 88, with 4 rows of 128 bytes 85, with 2 86.
+constexpr int MOVE_ROWS = 4, MOVE_PIECES = 16;
 __global__ __launch_bounds__(256) void pages_move_kernel(pi0_pages p, PlanSpace ws, const int* keep_all, int keep_stride) {
   const int s = blockIdx.y;
   const Move m = ws.moves[s];
   if (m.begin >= m.end) return;
-  const int pieces = p.kv_heads * p.head_dim / 8, groups = div_up(pieces, 32);
+  const int pieces = p.kv_heads * p.head_dim / 8, groups = div_up(pieces, MOVE_PIECES);
   const int group = blockIdx.x % groups, layer = blockIdx.x / groups >> 1;
   char* pool = reinterpret_cast<char*>((blockIdx.x / groups & 1) ? p.d_v : p.d_k) + 2 * layer * p.layer_stride;
-  const int wide = min(32, pieces - group * 32), deep = 256 / wide;
-  const int row = threadIdx.x / wide, piece = group * 32 + threadIdx.x % wide;
+  const int wide = min(MOVE_PIECES, pieces - group * MOVE_PIECES), deep = 256 / wide;
+  const int row = threadIdx.x / wide, piece = group * MOVE_PIECES + threadIdx.x % wide;
   const int per_head = p.head_dim / 8;
   pool += 2 * ((piece / per_head) * p.head_stride + (piece % per_head) * 8);
   const int* now = p.d_table + (size_t)s * p.max_pages;
@@ -457,7 +459,7 @@ bool workspace_ok(const pi0_pages* p, void* ws, size_t bytes, int* rc) {
 }
 
 hipError_t launch_move(hipStream_t s, const pi0_pages& p, const PlanSpace& ws, const int* keep, int keep_stride) {
-  const int groups = div_up(p.kv_heads * p.head_dim / 8, 32);
+  const int groups = div_up(p.kv_heads * p.head_dim / 8, MOVE_PIECES);
   hipLaunchKernelGGL(pages_move_kernel, dim3(groups * p.layers * 2, p.n_seqs), dim3(256), 0, s, p, ws, keep, keep_stride);
   return hipGetLastError();
 }
