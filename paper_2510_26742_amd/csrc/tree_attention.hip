@@ -121,9 +121,9 @@ struct RowState {
 __device__ __forceinline__ float dot_ones(bf16x2 w, float c) { return __builtin_amdgcn_fdot2_f32_bf16(w, bf16x2{(bf16)1.0f, (bf16)1.0f}, c, false); }
 __device__ __forceinline__ float dot_ones(f16x2 w, float c) { return __builtin_amdgcn_fdot2(w, f16x2{(f16)1.0f, (f16)1.0f}, c, false); }
 
-// o *= c, where it is: in the accumulation registers.  Written as a product, the sums are copied to vector registers in every round, whether
-// or not the branch is taken (64 instructions at D = 256).  The products that wrote them have long ended - the scores
-// that decided the branch are a later product's - and the waits in front and behind cover the longest there is.
+// o *= c, where it is: in the accumulation registers.  Written as a product, the sums are copied to vector registers in every granule, whether
+// or not the branch is taken (64 instructions at D = 256).  The products that wrote them may stand right in front: the wait
+// there, 64 cycles, is several times what the last of them takes, the one behind covers a product that reads what was written.
 template <int N>
 __device__ __forceinline__ void scale_sums(f32x4 (&o)[N], float c) {
   asm volatile("s_nop 15\n\ts_nop 15\n\ts_nop 15\n\ts_nop 15" ::: "memory");
@@ -334,12 +334,13 @@ __global__ __launch_bounds__(64 * RW, D < 256 || R == 1 ? 2 : 1) void tree_atten
         off[i] = (my_row + key) * (unsigned)(2 * p.token_stride) + ((of_v ? piece_v0 : piece_k0) ^ (of_v ? turn_v : turn_k)) * 16 - i * 1024;
       }
       if constexpr (BURST == 2)
-        asm volatile("s_add_u32 m0, %0, %4\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %3\n\tglobal_load_lds_dwordx4 %2, %3 offset:1024"
-                     ::"s"(at.to), "v"(off[0]), "v"(off[1]), "s"(at.from), "n"(burst * BURST * 1024) : "memory", "scc");
+        asm volatile("s_add_u32 m0, %0, %4\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %3\n\tglobal_load_lds_dwordx4 %2, %3 offset:%5"
+                     ::"s"(at.to), "v"(off[0]), "v"(off[1]), "s"(at.from), "n"(burst * BURST * 1024), "n"(1024) : "memory", "scc");
       else
-        asm volatile("s_add_u32 m0, %0, %6\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %5\n\tglobal_load_lds_dwordx4 %2, %5 offset:1024\n\t"
-                     "global_load_lds_dwordx4 %3, %5 offset:2048\n\tglobal_load_lds_dwordx4 %4, %5 offset:3072"
-                     ::"s"(at.to), "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(at.from), "n"(burst * BURST * 1024) : "memory", "scc");
+        asm volatile("s_add_u32 m0, %0, %6\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %5\n\tglobal_load_lds_dwordx4 %2, %5 offset:%7\n\t"
+                     "global_load_lds_dwordx4 %3, %5 offset:%8\n\tglobal_load_lds_dwordx4 %4, %5 offset:%9"
+                     ::"s"(at.to), "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(at.from), "n"(burst * BURST * 1024), "n"(1024), "n"(2 * 1024),
+                     "n"(3 * 1024) : "memory", "scc");
     };
     auto request = [&](int granule, int stage, int page0, int page1) {
       const Quarter at = quarter_of(granule, stage, page0, page1);
