@@ -300,6 +300,37 @@ def test_pool_beyond_32_bits():
     assert torch.equal(v[0, 33000, 600 - 512], rows[1][1])
 
 
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_rows_as_far_apart_as_is_taken(d):
+    """16 rows of a page 2^27 - 8 elements apart: the last offset inside a granule just fits 32 bits."""
+    apart, rng = (1 << 27) - 8, np.random.default_rng(d)
+    pools = [torch.empty(2 * 16 * apart, dtype=torch.bfloat16, device=DEV).as_strided((1, 2, 16, 1, d), (32 * apart, 16 * apart, apart, d, 1)) for _ in range(2)]
+    held = [torch.from_numpy(rng.standard_normal((32, 1, d))).to(DEV, torch.bfloat16) for _ in range(2)]
+    for t, x in zip(pools, held):
+        t[0, 1], t[0, 0] = x[:16], x[16:]                       # the list is pages 1, 0
+    pages = binding.Pages(*pools, ints([[1, 0]]), ints([29]), ints([1, 1]))
+    q = torch.from_numpy(rng.standard_normal((3, 2, d))).to(DEV, torch.bfloat16)
+    got = f64(binding.pi0_tree_attention(pages, 0, q, ints([0, 3]), 3))
+    see = np.concatenate([np.ones((3, 29), dtype=bool), np.tril(np.ones((3, 3), dtype=bool))], 1)
+    k, v = (f64(x) for x in held)
+    want = paged.attention(f64(q), k, v, see, d ** -0.5)
+    score = d ** -0.5 * np.sqrt((f64(q) ** 2).sum(-1).max() * (k ** 2).sum(-1).max())
+    bar = (3 * 2.0 ** -8 + 2.0 ** -24 * (2 * (d + 2) * score + 64)) * np.abs(v).max()
+    assert np.abs(got - want).max() <= bar
+
+
+@pytest.mark.parametrize("seqs,count,heads,kv_heads,d", [(1, 70, 4, 1, 256), (4, 70, 4, 1, 128), (6, 33, 16, 4, 64)])
+def test_results_in_the_place_of_the_queries(seqs, count, heads, kv_heads, d):
+    """Several tiles of rows per sequence, units that one block has all of and units that many have a part in: the same bits."""
+    c = Case(80, [2500, 10, 300, 64, 0, 31][:seqs], [count - 5 * s for s in range(seqs)], heads, kv_heads, d, 32, "bf16")
+    c.run()
+    c.check()
+    q = c.q.clone()
+    binding.pi0_tree_attention(c.pages, c.layer, q, ints(c.starts), c.most, mask=c.mask, out=q)
+    mine = slice(int(c.starts[0]), int(c.starts[-1]))
+    assert torch.equal(q[mine], c.out[mine]) and torch.equal(q[:c.before], c.q[:c.before]) and torch.equal(q[mine.stop:], c.q[mine.stop:])
+
+
 def test_streams_and_replays():
     """Calls on two streams at once, and a graph replayed with other lengths, masks and pages, against eager calls bit for bit."""
     a, b = Case(101, [900, 40], [3, 9], 8, 1, 256, 32, "bf16"), Case(102, [50, 1200, 7], [20, 1, 2], 16, 4, 128, 16, "f16")
