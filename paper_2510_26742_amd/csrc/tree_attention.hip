@@ -298,13 +298,6 @@ __global__ __launch_bounds__(64 * RW, D < 256 || R == 1 ? 2 : 1) void tree_atten
 #pragma unroll
       for (int i = 0; i < STEPS; i++) q[n][i] = *reinterpret_cast<const s16x8*>(q_row + i * 32);
     }
-    if (a.odd_scale) {
-#pragma unroll
-      for (int n = 0; n < R; n++) {
-#pragma unroll
-        for (int i = 0; i < STEPS; i++) q[n][i] = (q[n][i] ^ a.negate) & a.q_bits;
-      }
-    }
     const char* const pool_k = reinterpret_cast<const char*>(p.d_k) + 2 * (a.layer + kv_head * p.head_stride);
     const char* const pool_v = reinterpret_cast<const char*>(p.d_v) + 2 * (a.layer + kv_head * p.head_stride);
 
@@ -360,8 +353,7 @@ __global__ __launch_bounds__(64 * RW, D < 256 || R == 1 ? 2 : 1) void tree_atten
       st[n].shift = 0.f;
       st[n].l = 0.f;
     }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // from here on only the tiles' requests are in flight
-    __syncthreads();                                   // what was in the tiles has been read
+    __syncthreads();   // what was in the tiles has been read
     unsigned none = 0;   // two bits per granule, the latest requested lowest: its first, last 16 keys are on no page
     int page0, page1;
     auto next_pages = [&] {
@@ -375,6 +367,19 @@ __global__ __launch_bounds__(64 * RW, D < 256 || R == 1 ? 2 : 1) void tree_atten
       if (AHEAD || g0 + i < g1) request(in_unit(g0 + i), i, page0, page1);
     }
     next_entries(in_unit(g0 + STAGES - 1));
+    // The queries have been on their way with the first tiles.  (All are waited for here, once, and not by the first product in the loop.)
+#pragma unroll
+    for (int n = 0; n < R; n++) {
+#pragma unroll
+      for (int i = 0; i < STEPS; i++) asm volatile("" : "+v"(q[n][i]));
+    }
+    if (a.odd_scale) {
+#pragma unroll
+      for (int n = 0; n < R; n++) {
+#pragma unroll
+        for (int i = 0; i < STEPS; i++) q[n][i] = (q[n][i] ^ a.negate) & a.q_bits;
+      }
+    }
 
     int odd_from = g1;   // first granule with such values
     // A weight of zero does not silence an infinity or a NaN.  Committed values are seen by every row; where there is anything
