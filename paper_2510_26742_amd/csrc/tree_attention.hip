@@ -50,11 +50,13 @@ struct Mat<f16> {
 // than it is - what a block spends before a unit's first granule and behind its last -, and a run, LEAST long at least, may end one
 // unit, hold others and begin the next.  A block writes a unit that it has all of; of any other it leaves a partial result, in slot 1 if it
 // has the first granule, in slot 0 if not, and the second launch joins them.
-// LEAST: of few keys, 1 or 2 make more partial results than their reading at once is worth (4 x 8 tokens over up to 4096, 8 heads over 1 of
-// 256: 19.6 us with 1, 15.2 with 2, 14.1 with 3), many take longer one behind the other (1 token over 816: 8.7, 9.5, 9.4, with 4 10.9).
+// LEAST: of few keys, runs of 1 or 2 make more partial results than their reading at once is worth (4 x 8 tokens over up to 4096, 8 heads over
+// 1 of 256: 19.6 us with 1, 15.2 with 2, 14.1 with 3), long ones take their time one granule behind the other (1 token over 816: 8.7, 9.5, 9.4, with 4
+// 10.9).  A tile that is full, 64 rows or more, has partial results of twice and four times the bytes: LEAST_FULL (1 x 16 over 1024 / 4096 / 16384
+// 11.8 / 14.1 / 21.8 us with 3, 11.9 / 13.7 / 20.3 with 4, 13.9 / 14.5 / 18.4 with 6; of 84 such cases the mean is 18.3, 18.0, 18.1).
 // START: 12 costs short units up to 4 %, 2 lets row tiles of the same keys drift apart, so that each fetches them for itself (8 x 64 over
 // 16384 in tiles of 64 rows: 75.8 us with 2, 61.9 with 6).
-constexpr int GRANULE = 32, START = 6, LEAST = 3;
+constexpr int GRANULE = 32, START = 6, LEAST = 3, LEAST_FULL = 4;
 
 // A stage of K and V tiles is 128 D bytes; STAGES of them per block.  BLOCKS: as many as the chip's 256 compute units hold at once, two
 // to each where registers let them: one reads while another begins or ends a unit or waits for its waves.  Heads of 64 have so little
@@ -222,7 +224,7 @@ __global__ __launch_bounds__(64 * RW, D < 256 || R == 1 ? 2 : 1) void tree_atten
       before = __builtin_amdgcn_readlane(end, 63);
     }
     line = before;
-    run = max(LEAST, div_up(line, BLOCKS));
+    run = max(a.sets < 4 ? LEAST : LEAST_FULL, div_up(line, BLOCKS));
     if (blockIdx.x == 0 && threadIdx.x == 0) *a.run = run;
     if (p.n_seqs > 64) __syncthreads();
   }
