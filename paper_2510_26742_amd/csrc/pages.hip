@@ -150,7 +150,8 @@ struct PlanArgs {
 // to - those are replaced -, the list has `want` pages afterwards, of which it holds `held` now.  reserve: want >= held,
 // compact: want <= held.  What bounds it is trips to memory (0.6 us each) and 16 waves for all sequences, so: numbers
 // that all sequences have are read at once, a list and the positions that it keeps in one trip, reference counts in a second, and what
-// was found is left in the workspace for the second half.  The free pages cost one trip per 1024 reference counts until enough are found.
+// was found is left in the workspace for the second half (4 sequences 5.8 us for a compaction and 4.6 for a reservation, 48 with 560 positions each
+// 12.9 and 7.8).  The free pages cost one trip per 1024 reference counts until enough are found.
 template <int KIND>
 __global__ __launch_bounds__(PLAN_THREADS) void pages_plan_kernel(PlanArgs a) {
   const pi0_pages& p = a.p;
@@ -336,6 +337,7 @@ __global__ __launch_bounds__(256) void pages_move_kernel(pi0_pages p, PlanSpace 
   }
 }
 
+// A wave per pair, everything checked before anything is written.  Bound by four trips to memory: 2.9 us for 3 continuations, 5.0 for 32.
 __global__ __launch_bounds__(PLAN_THREADS) void pages_fork_kernel(pi0_pages p, const int* src, const int* dst, int n) {
   __shared__ int s_mark[MAX_SEQS], s_src[MAX_SEQS], s_dst[MAX_SEQS], s_bad;
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
@@ -388,7 +390,8 @@ __device__ int own_pages(const pi0_pages& p, int seq, int tokens) {
 
 // One block: 32 tokens of one layer between the fragment order that the attention kernels of the pass read (32 keys x 256 per
 // 16 KiB chunk; values transposed) and rows of pages.  Rows are 512 bytes, fragments 16-byte pieces of one key or, of the
-// values, of 8 keys at one d: those pass through shared memory.
+// values, of 8 keys at one d: those pass through shared memory.  Bound by memory and the way there: 816 tokens of 18 layers, 30 MB read and
+// written, 9.0 us to pages and 7.5 us back.
 constexpr int CHUNK = 32, VROW = 256 + 8;
 __device__ __forceinline__ bf16* page_row(const pi0_pages& p, void* pool, int layer, int seq, int pos) {
   const int page = page_at(p, seq, pos / p.page_tokens);
