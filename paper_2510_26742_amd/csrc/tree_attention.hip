@@ -8,9 +8,9 @@
 // maxima need two exchanges between the quarters of a wave.  V^T is read out of row-major tiles with the transposing LDS
 // load (4 keys x 16 d per 16 lanes).  A wave has R times 16 rows: what it reads of K and V out of LDS serves all of them.  R = 1 where
 // the cache's own bytes are what the time goes to, 2 where rows are many.
-// What bounds it: few rows the reads of the cache (64 x 1 token, 8 heads over 1 of 256, up to 8192 keys: 277 MB in 43 us, 6.4 TB/s);
-// many rows the issue of instructions, of which a wave that is alone on its SIMD has one per 4 cycles (8 x 64 nodes over 16384: 25.7
-// GFLOP in 49 us, 525 TFLOP/s; a granule's 64 products per wave could end in 1024 cycles, but stand among 350 instructions), which is why the loop does nothing that
+// What bounds it: few rows the reads of the cache (64 x 1 token, 8 heads over 1 of 256, up to 8192 keys: 277 MB in 43.6 us, 6.4 TB/s);
+// many rows the issue of instructions, of which a wave that is alone on its SIMD has one per 4 cycles (8 x 64 nodes over 16384: 25.8
+// GFLOP in 48 us, 540 TFLOP/s; a granule's 64 products per wave could end in 1024 cycles, but stand among 350 instructions), which is why the loop does nothing that
 // can be done in front of it.
 // Tiles come straight into LDS, 16 bytes per lane; the pieces of a row are permuted by its key (on the global side: a lane
 // may fetch any piece) so that neither product's reads collide in the banks.
