@@ -287,14 +287,16 @@ __global__ __launch_bounds__(64 * RW, D < 256 || R == 1 ? 2 : 1) void tree_atten
     int node[R], head[R];
     bool live[R];
     const unsigned* mask[R];
-    s16x8 q[R][STEPS];   // (a lane without a row takes the first token's, and gives nothing back)
+    // A lane without a row takes its tile's last one and gives nothing back: scores that its wave has anyway, so it moves no reference of the
+    // others, and no other block's row, which may be its result by now (out may be q).
+    s16x8 q[R][STEPS];
 #pragma unroll
     for (int n = 0; n < R; n++) {
-      const int r = row_tile * ROWS + (rw * R + n) * 16 + kkey;
-      live[n] = r < rows.y * a.group;
+      const int place = row_tile * ROWS + (rw * R + n) * 16 + kkey, r = min(place, rows.y * a.group - 1);
+      live[n] = place == r;
       // r / group: both below 2^20, and half a row is more than the reciprocal is off by
-      node[n] = live[n] ? (int)(((float)r + 0.5f) * __builtin_amdgcn_rcpf((float)a.group)) : 0;
-      head[n] = kv_head * a.group + (live[n] ? r - node[n] * a.group : 0);
+      node[n] = (int)(((float)r + 0.5f) * __builtin_amdgcn_rcpf((float)a.group));
+      head[n] = kv_head * a.group + r - node[n] * a.group;
       mask[n] = a.mask + (size_t)(rows.x + node[n]) * a.mask_words;
       const T* const q_row = reinterpret_cast<const T*>(a.q) + (rows.x + node[n]) * a.q_row_stride + head[n] * a.q_head_stride + quad * 8;
 #pragma unroll

@@ -380,3 +380,36 @@ def test_binding_refuses():
         with pytest.raises(binding.Pi0Error) as e:
             binding.pi0_tree_attention(c.pages, a["layer"], a["q"], a["s"], a["most"], **kw)
         assert e.value.code == binding.PI0_EINVAL, bad
+
+
+@pytest.mark.parametrize("seqs,count,heads,kv_heads,d", [(1, 70, 4, 1, 256), (1, 33, 4, 1, 128), (4, 70, 4, 1, 256), (4, 70, 4, 1, 64)])
+def test_lanes_without_a_row_have_no_say(seqs, count, heads, kv_heads, d):
+    """The last tile has fewer rows than lanes.  What the first token asks for - scores that grow along the keys, time and again - is nothing
+    to the rows of other waves: the same bits whether it does or not."""
+    print("[gpu] tree_attention idle lanes", seqs, count, d, flush=True)
+    c = Case(120 + d, [2500, 10, 300, 64][:seqs], [count - 5 * s for s in range(seqs)], heads, kv_heads, d, 32, "bf16", kind="chain")
+    c.run()
+    want = c.out.clone()
+    for s in range(seqs):
+        c.q[c.starts[s]] *= 40
+    c.run()
+    c.check()
+    for s in range(seqs):
+        rest = slice(int(c.starts[s]) + 32 // heads, int(c.starts[s + 1]))      # 32 rows: the first wave's
+        assert torch.equal(c.out[rest].view(torch.int16), want[rest].view(torch.int16))
+
+
+@pytest.mark.parametrize("d,dtype", [(256, "bf16"), (128, "f16"), (64, "bf16")])
+def test_in_place_where_blocks_have_many_units(d, dtype):
+    """Two tiles of rows for each of 600 short sequences, the second hardly filled, sharp scores: a block has several units, and the first tile's
+    results take their queries' place while others are at the second.  The same bits as beside them, time after time."""
+    print("[gpu] tree_attention in place, many units", d, dtype, flush=True)
+    rng = np.random.default_rng(d)
+    c = Case(130, rng.integers(0, 48, 600).tolist(), [17] * 600, 8, 1, d, 16, dtype, spread=30.0)
+    c.run()
+    mine, starts = slice(int(c.starts[0]), int(c.starts[-1])), ints(c.starts)
+    for _ in range(4):
+        q = c.q.clone()
+        binding.pi0_tree_attention(c.pages, c.layer, q, starts, c.most, mask=c.mask, out=q)
+        assert torch.equal(q[mine].view(torch.int16), c.out[mine].view(torch.int16))
+        assert torch.equal(q[:c.before], c.q[:c.before]) and torch.equal(q[mine.stop:], c.q[mine.stop:])
