@@ -15,6 +15,8 @@
  * pi0_pages_status, which waits, and store and load, which go by what the ctx holds at the time of the call and refuse a stream that is
  * being captured (PI0_EHIP, hipErrorIllegalState).  Calls that overlap in time must not share a workspace, nor may one change a cache that
  * another reads; a graph keeps the addresses it was captured with, its workspace included.
+ * PI0_EHIP is a failure of the call's own launches, whatever error an earlier call of the caller's has left; a part of the work may
+ * have run by then, and a cache that pi0_pages_reserve or _compact was to change is no longer to be used.
  * Results do not depend on what else runs: no sums by atomics, pages are handed out in one fixed order.
  */
 #ifndef PI0_OPS_H

@@ -463,19 +463,16 @@ bool workspace_ok(const pi0_pages* p, void* ws, size_t bytes, int* rc) {
 
 hipError_t launch_move(hipStream_t s, const pi0_pages& p, const PlanSpace& ws, const int* keep, int keep_stride) {
   const int groups = div_up(p.kv_heads * p.head_dim / 8, MOVE_PIECES);
-  hipLaunchKernelGGL(pages_move_kernel, dim3(groups * p.layers * 2, p.n_seqs), dim3(256), 0, s, p, ws, keep, keep_stride);
-  return hipGetLastError();
+  return enqueue(s, dim3(groups * p.layers * 2, p.n_seqs), 256, pages_move_kernel, p, ws, keep, keep_stride);
 }
 
 }  // namespace
 
 hipError_t launch_pages_store(hipStream_t s, const pi0_pages& p, int seq, const bf16* kc, const bf16* vc, size_t k_layer, size_t v_layer, int tokens) {
-  hipLaunchKernelGGL(pages_store_kernel, dim3(div_up(tokens, CHUNK), p.layers), dim3(256), 0, s, p, seq, kc, vc, k_layer, v_layer, tokens);
-  return hipGetLastError();
+  return enqueue(s, dim3(div_up(tokens, CHUNK), p.layers), 256, pages_store_kernel, p, seq, kc, vc, k_layer, v_layer, tokens);
 }
 hipError_t launch_pages_load(hipStream_t s, const pi0_pages& p, int seq, bf16* kc, bf16* vc, size_t k_layer, size_t v_layer, int tokens) {
-  hipLaunchKernelGGL(pages_load_kernel, dim3(div_up(tokens, CHUNK), p.layers), dim3(256), 0, s, p, seq, kc, vc, k_layer, v_layer, tokens);
-  return hipGetLastError();
+  return enqueue(s, dim3(div_up(tokens, CHUNK), p.layers), 256, pages_load_kernel, p, seq, kc, vc, k_layer, v_layer, tokens);
 }
 
 extern "C" {
@@ -490,8 +487,7 @@ int pi0_pages_reserve(const pi0_pages* pages, const int32_t* d_extra, void* d_wo
   a.p = *pages;
   a.ws = plan_space(*pages, d_workspace);
   a.extra = d_extra;
-  hipLaunchKernelGGL(pages_plan_kernel<PLAN_RESERVE>, dim3(1), dim3(PLAN_THREADS), 0, s, a);
-  hipError_t e = hipGetLastError();
+  hipError_t e = enqueue(s, dim3(1), PLAN_THREADS, pages_plan_kernel<PLAN_RESERVE>, a);
   if (e == hipSuccess) e = launch_move(s, *pages, a.ws, nullptr, 0);
   return e == hipSuccess ? PI0_OK : PI0_EHIP;
 }
@@ -510,8 +506,7 @@ int pi0_pages_compact(const pi0_pages* pages, const int32_t* d_start, const int3
   a.keep = d_keep;
   a.n_keep = d_n_keep;
   a.keep_stride = keep_stride;
-  hipLaunchKernelGGL(pages_plan_kernel<PLAN_COMPACT>, dim3(1), dim3(PLAN_THREADS), 0, s, a);
-  hipError_t e = hipGetLastError();
+  hipError_t e = enqueue(s, dim3(1), PLAN_THREADS, pages_plan_kernel<PLAN_COMPACT>, a);
   if (e == hipSuccess) e = launch_move(s, *pages, a.ws, d_keep, keep_stride);
   return e == hipSuccess ? PI0_OK : PI0_EHIP;
 }
@@ -519,8 +514,7 @@ int pi0_pages_compact(const pi0_pages* pages, const int32_t* d_start, const int3
 int pi0_pages_fork(const pi0_pages* pages, const int32_t* d_src, const int32_t* d_dst, int n, void* hip_stream) {
   if (!pages_ok(pages) || d_src == nullptr || d_dst == nullptr || n < 1 || n > pages->n_seqs) return PI0_EINVAL;
   hipStream_t s = reinterpret_cast<hipStream_t>(hip_stream);
-  hipLaunchKernelGGL(pages_fork_kernel, dim3(1), dim3(PLAN_THREADS), 0, s, *pages, d_src, d_dst, n);
-  return hipGetLastError() == hipSuccess ? PI0_OK : PI0_EHIP;
+  return enqueue(s, dim3(1), PLAN_THREADS, pages_fork_kernel, *pages, d_src, d_dst, n) == hipSuccess ? PI0_OK : PI0_EHIP;
 }
 
 int pi0_pages_status(const pi0_pages* pages, void* hip_stream) {

@@ -12,6 +12,17 @@ bool pages_ok(const pi0_pages* p);
 // rows of `heads` heads (0: any number) of `head_dim` elements in type `dtype`
 bool rows_ok(const pi0_rows* r, int heads, int head_dim, int dtype);
 
+// A launch and its own result: hipGetLastError would give back an error that an earlier call of the caller's left, too.
+template <class T>
+struct Same { typedef T type; };
+template <class... P>
+static inline hipError_t enqueue(hipStream_t s, dim3 grid, int threads, void (*kernel)(P...), const typename Same<P>::type&... arg) {
+  void* args[] = {const_cast<void*>(static_cast<const void*>(&arg))...};
+  const hipError_t e = hipLaunchKernel(reinterpret_cast<const void*>(kernel), grid, dim3(threads), args, 0, s);
+  if (e != hipSuccess) (void)hipGetLastError();   // told by what is returned
+  return e;
+}
+
 static __host__ __device__ __forceinline__ int div_up(int a, int b) { return (a + b - 1) / b; }
 
 // the page behind entry `idx` of a sequence's list, or -1

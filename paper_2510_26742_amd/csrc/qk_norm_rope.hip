@@ -130,15 +130,14 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(NormRopeArgs a) {
 }
 
 template <class T, class X, int D>
-void launch(hipStream_t s, const NormRopeArgs& a) {
-  const dim3 grid(ceil_div(a.max_rows, 4), a.p.n_seqs);
-  hipLaunchKernelGGL((qk_norm_rope_kernel<T, X, D>), grid, dim3(256), 0, s, a);
+hipError_t launch(hipStream_t s, const NormRopeArgs& a) {
+  return enqueue(s, dim3(div_up(a.max_rows, 4), a.p.n_seqs), 256, qk_norm_rope_kernel<T, X, D>, a);
 }
 template <class T, class X>
-void launch_dim(hipStream_t s, const NormRopeArgs& a) {
-  if (a.p.head_dim == 64) launch<T, X, 64>(s, a);
-  else if (a.p.head_dim == 128) launch<T, X, 128>(s, a);
-  else launch<T, X, 256>(s, a);
+hipError_t launch_dim(hipStream_t s, const NormRopeArgs& a) {
+  if (a.p.head_dim == 64) return launch<T, X, 64>(s, a);
+  if (a.p.head_dim == 128) return launch<T, X, 128>(s, a);
+  return launch<T, X, 256>(s, a);
 }
 
 }  // namespace
@@ -181,12 +180,8 @@ extern "C" int pi0_qk_norm_rope(const pi0_pages* pages, int layer, const pi0_row
   const double step = rope_dim > 0 ? -2.0 * log(rope_base) / rope_dim : 0.0;
   for (int i = 0; i < rope_dim / 2; i++) a.turns[i] = exp(i * step) / (2.0 * M_PI);
   hipStream_t s = reinterpret_cast<hipStream_t>(hip_stream);
-  if (pages->dtype == PI0_BF16) {
-    if (type == PI0_F32) launch_dim<bf16, float>(s, a);
-    else launch_dim<bf16, bf16>(s, a);
-  } else {
-    if (type == PI0_F32) launch_dim<f16, float>(s, a);
-    else launch_dim<f16, f16>(s, a);
-  }
-  return hipGetLastError() == hipSuccess ? PI0_OK : PI0_EHIP;
+  hipError_t e;
+  if (pages->dtype == PI0_BF16) e = type == PI0_F32 ? launch_dim<bf16, float>(s, a) : launch_dim<bf16, bf16>(s, a);
+  else e = type == PI0_F32 ? launch_dim<f16, float>(s, a) : launch_dim<f16, f16>(s, a);
+  return e == hipSuccess ? PI0_OK : PI0_EHIP;
 }

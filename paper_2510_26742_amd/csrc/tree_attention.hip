@@ -760,10 +760,10 @@ Space space_of(const pi0_pages& p, int heads, int max_rows) {
 }
 
 template <class T>
-void launch(hipStream_t s, TreeArgs& a, char* ws) {
-  with_dim(a.p.head_dim, [&](auto d) {
+hipError_t launch(hipStream_t s, TreeArgs& a, char* ws) {
+  return with_dim(a.p.head_dim, [&](auto d) {
     const int rows = a.max_rows * a.group;
-    with_rows(rows, a.p.n_seqs * a.p.kv_heads, [&](auto r) {
+    return with_rows(rows, a.p.n_seqs * a.p.kv_heads, [&](auto r) {
       constexpr int D = d, R = r, BLOCKS = Shape<D, R>::BLOCKS;
       const Space at = space_of<D, R>(a.p, rows);
       a.sets = at.sets;
@@ -771,16 +771,14 @@ void launch(hipStream_t s, TreeArgs& a, char* ws) {
       a.part_ml = reinterpret_cast<float2*>(ws + at.part_ml);
       a.upto = reinterpret_cast<int*>(ws + at.upto);
       a.run = reinterpret_cast<int*>(ws + at.run);
-      hipLaunchKernelGGL((tree_attention_kernel<T, D, R>), dim3(BLOCKS), dim3(64 * RW), 0, s, a);
+      const hipError_t e = enqueue(s, dim3(BLOCKS), 64 * RW, tree_attention_kernel<T, D, R>, a);
+      if (e != hipSuccess) return e;
       const int units = a.p.n_seqs * a.p.kv_heads * div_up(rows, 16 * R * RW);
       const int items = div_up(rows, 16) * (D / 16);   // of 16 rows and 16 d
       if (units <= BLOCKS / 16)
-        hipLaunchKernelGGL((tree_merge_kernel<T, D, R, 8>), dim3(items, a.p.kv_heads, a.p.n_seqs), dim3(512), 0, s, a);
-      else
-        hipLaunchKernelGGL((tree_merge_kernel<T, D, R, 1>), dim3(div_up(items, 8), a.p.kv_heads, a.p.n_seqs), dim3(512), 0, s, a);
-      return 0;
+        return enqueue(s, dim3(items, a.p.kv_heads, a.p.n_seqs), 512, tree_merge_kernel<T, D, R, 8>, a);
+      return enqueue(s, dim3(div_up(items, 8), a.p.kv_heads, a.p.n_seqs), 512, tree_merge_kernel<T, D, R, 1>, a);
     });
-    return 0;
   });
 }
 
@@ -832,9 +830,9 @@ int pi0_tree_attention(const pi0_pages* pages, int layer, const pi0_rows* q, con
   }
   a.layer = layer * pages->layer_stride;
   hipStream_t s = reinterpret_cast<hipStream_t>(hip_stream);
-  if (pages->dtype == PI0_BF16) launch<bf16>(s, a, reinterpret_cast<char*>(d_workspace));
-  else launch<f16>(s, a, reinterpret_cast<char*>(d_workspace));
-  return hipGetLastError() == hipSuccess ? PI0_OK : PI0_EHIP;
+  char* const ws = reinterpret_cast<char*>(d_workspace);
+  const hipError_t e = pages->dtype == PI0_BF16 ? launch<bf16>(s, a, ws) : launch<f16>(s, a, ws);
+  return e == hipSuccess ? PI0_OK : PI0_EHIP;
 }
 
 }  // extern "C"

@@ -252,3 +252,56 @@ def test_captured_and_replayed_beside_eager_calls():
         gpu.pi0_pages_compact(None, ints([-1] * 5 + [0]), start=ints([0] * 6))      # eager, in between
         cpu.compact(None, [-1] * 5 + [0], [0] * 6)
         same(gpu, cpu, f"eager {step}")
+
+
+def hip_error_left(code=12345):
+    """An error that a call of the caller's own left in this thread (a device that is none), and the runtime's way to fetch it."""
+    import ctypes
+    hip = ctypes.CDLL(binding.LIB_PATH)
+    hip.hipSetDevice.argtypes, hip.hipSetDevice.restype = [ctypes.c_int], ctypes.c_int
+    hip.hipGetLastError.restype = ctypes.c_int
+    assert hip.hipSetDevice(code) != 0
+    return hip.hipGetLastError
+
+
+def test_an_error_left_by_the_caller_is_not_a_calls_own():
+    """Both halves of reserve and compact run, and every call says PI0_OK, although the thread's last error is another call's."""
+    gpu, cpu = make(10, layers=2, kv_heads=2)
+    grow(gpu, cpu, [40, 5, 0, 0, 0, 0])
+    src, dst, extra, n, start = ints([0]), ints([2]), ints([-1, -1, 3, -1, -1, -1]), ints([20, -1, -1, -1, -1, -1]), ints([0] * 6)
+    keep = ints([[2 * i for i in range(20)]] * 6)
+    ws = torch.empty(gpu._plan_bytes, dtype=torch.uint8, device=DEV)
+    q, k = torch.ones((1, 2, 64), dtype=torch.bfloat16, device=DEV), torch.ones((1, 2, 64), dtype=torch.bfloat16, device=DEV)
+    starts = ints([0, 1, 1, 1, 1, 1, 1])
+    rows = binding._rows(q, "q", 1, 2, 64)
+    room = binding.lib().pi0_tree_attention_workspace_bytes(gpu._ref, 2, 1, 1)
+    ws2, out = torch.empty(room, dtype=torch.uint8, device=DEV), torch.empty_like(q)
+    torch.cuda.synchronize()
+    L, ref, last = binding.lib(), gpu._ref, hip_error_left
+    calls = [lambda: L.pi0_pages_fork(ref, src.data_ptr(), dst.data_ptr(), 1, None),
+             lambda: L.pi0_pages_reserve(ref, extra.data_ptr(), ws.data_ptr(), gpu._plan_bytes, None),
+             lambda: L.pi0_pages_compact(ref, start.data_ptr(), keep.data_ptr(), 20, n.data_ptr(), ws.data_ptr(), gpu._plan_bytes, None)]
+    codes = []
+    for call in calls:
+        fetch = last()
+        codes.append(call())
+        fetch()
+    assert codes == [binding.PI0_OK] * 3
+    torch.cuda.synchronize()
+    cpu.fork([0], [2])
+    cpu.reserve([-1, -1, 3, -1, -1, -1])
+    cpu.compact([[2 * i for i in range(20)]] * 6, [20, -1, -1, -1, -1, -1], [0] * 6)
+    gpu.pi0_pages_status()
+    same(gpu, cpu)
+    gpu.pi0_pages_reserve(ints([1, -1, -1, -1, -1, -1]))
+    import ctypes
+    r, o = ctypes.byref(rows), ctypes.byref(binding._rows(out, "out", 1, 2, 64))
+    kr = ctypes.byref(binding._rows(k, "k", 1, 2, 64))
+    for call in (lambda: L.pi0_qk_norm_rope(ref, 0, r, kr, kr, o, starts.data_ptr(), 1, 1, None, None, None, 1.0, 1e-6, 64, 1e4, 0, None),
+                 lambda: L.pi0_tree_attention(ref, 0, r, o, starts.data_ptr(), 1, 1, None, 0, 0.125, ws2.data_ptr(), room, None)):
+        fetch = last()
+        code = call()
+        fetch()
+        assert code == binding.PI0_OK
+    torch.cuda.synchronize()
+    assert torch.isfinite(out.float()).all()
