@@ -51,7 +51,7 @@ typedef struct pi0_pages {
   int32_t* d_status;     /* [1], 0 at first: what pi0_pages_status reports                            */
   int64_t layer_stride, page_stride, token_stride, head_stride;
   int32_t dtype;         /* PI0_BF16 or PI0_F16                                                       */
-  int32_t layers;        /* >= 1                                                                      */
+  int32_t layers;        /* 1 .. 65536, layers * kv_heads * head_dim <= 2^29                          */
   int32_t n_pages;       /* 1 .. 2^24                                                                 */
   int32_t page_tokens;   /* 16, 32, 64, 128 or 256                                                    */
   int32_t kv_heads;      /* 1 .. 256                                                                  */

@@ -23,6 +23,8 @@ bool pages_ok(const pi0_pages* p) {
   if (p->kv_heads < 1 || p->kv_heads > 256) return false;
   if (p->head_dim != 64 && p->head_dim != 128 && p->head_dim != 256) return false;
   if (p->n_seqs < 1 || p->n_seqs > MAX_SEQS || p->max_pages < 1 || (int64_t)p->max_pages * p->page_tokens > 1 << 24) return false;
+  // (the moves' grid, a block of 256 threads per 128 elements of a layer, has less than 2^32 threads)
+  if ((int64_t)p->layers * p->kv_heads * p->head_dim > 1 << 29) return false;
   if (p->token_stride >= (int64_t)1 << 27) return false;
   // strides: whole 16-byte pieces, and, from the innermost axis outwards, each axis beyond all that lies inside it
   int64_t stride[4] = {p->layer_stride, p->page_stride, p->token_stride, p->head_stride};

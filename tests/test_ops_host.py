@@ -245,3 +245,18 @@ def test_plain_attention_against_torch():
     want = torch.nn.functional.scaled_dot_product_attention(*t, attn_mask=torch.from_numpy(seen), scale=0.3).transpose(0, 1).numpy()
     alive = [0, 1, 3, 4]
     assert np.allclose(got[alive], want[alive]) and not got[2].any()
+
+
+def test_layers_that_one_launch_can_move(L):
+    """A move has a block of 256 threads per 128 elements of a layer's keys and of its values: more than fit one launch are refused, at the
+    door and not behind the plan."""
+    def wide(**kw):
+        c = dict(kv_heads=256, head_dim=256, token_stride=1 << 16, page_stride=1 << 20, page_tokens=16, n_pages=1, layers=1 << 13, layer_stride=1 << 20)
+        return ctypes.byref(good(**{**c, **kw}))
+    assert L.pi0_pages_workspace_bytes(wide()) > 0
+    for kw in (dict(layers=(1 << 13) + 1), dict(layers=1 << 16), dict(layers=(1 << 16) + 1, kv_heads=1, head_dim=64)):
+        assert L.pi0_pages_workspace_bytes(wide(**kw)) == 0, kw
+        assert L.pi0_pages_reserve(wide(**kw), FAKE, FAKE, 1 << 40, None) == binding.PI0_EINVAL
+        assert L.pi0_pages_compact(wide(**kw), None, FAKE, 1, FAKE, FAKE, 1 << 40, None) == binding.PI0_EINVAL
+    # the grid of the largest that is taken: blocks of 128 elements, keys and values
+    assert (1 << 29) // 128 * 2 * 256 + 2 * 256 * (1 << 16) < 1 << 32
