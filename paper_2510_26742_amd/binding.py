@@ -445,8 +445,9 @@ class Pages:
 
     def _on(self, stream, *tensors):
         """(stream handle, context) of a call: inside the context the cache's device is the current one and the call's stream (None: the
-        device's default stream) torch's, so that scratch is allocated in the stream's order.  Tensors that belong to another
-        stream than the call's stay allocated until the call has run, also if the caller drops them."""
+        device's default stream) torch's, so that scratch is allocated in the stream's order.  What a call on another stream than the default
+        one is given stays allocated until it has run, also if the caller drops it.  (Where the default stream is torch's current one and the
+        call's, tensors that another stream allocated are the caller's to keep, as with any torch operation: looking after each costs 0.3 us.)"""
         import torch
         index = self._index
         for t in tensors:
@@ -455,8 +456,9 @@ class Pages:
         handle = 0 if stream is None else stream.cuda_stream
         if stream is not None and stream.device_index != index:
             _refuse(f"a stream of {self.device} expected")
-        if torch._C._cuda_getCurrentRawStream(index) == handle and torch._C._cuda_getDevice() == index:
-            return handle or None, _nothing
+        current = torch._C._cuda_getCurrentRawStream(index) == handle and torch._C._cuda_getDevice() == index
+        if current and handle == 0:
+            return None, _nothing
         s = torch.cuda.default_stream(self.device) if stream is None else stream
         for t in tensors:
             if t is not None:
@@ -465,7 +467,7 @@ class Pages:
             self._streams.add(handle)
             for t in (self.k, self.v, self.table, self.length, self.refs, self.status):
                 t.record_stream(s)
-        return handle or None, torch.cuda.stream(s)
+        return handle or None, _nothing if current else torch.cuda.stream(s)
 
     def _scratch(self, nbytes: int):
         import torch

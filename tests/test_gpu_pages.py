@@ -305,3 +305,33 @@ def test_an_error_left_by_the_caller_is_not_a_calls_own():
         assert code == binding.PI0_OK
     torch.cuda.synchronize()
     assert torch.isfinite(out.float()).all()
+
+
+@pytest.mark.parametrize("inside", [True, False])
+def test_what_a_call_was_given_stays_until_it_has_run(inside):
+    """Tensors of the default stream, given to a call on another (which is torch's current one, or is not) and dropped: while that stream has not
+    come to the call, their memory is not handed out again."""
+    gpu, cpu = make(11)
+    grow(gpu, cpu, [30, 30, 0, 0, 0, 0])
+    side = torch.cuda.Stream()
+    big = 300_001                                                     # a size that nothing else asks for
+    keep = torch.zeros((6, big), dtype=torch.int32, device=DEV)
+    keep[0, :10] = torch.arange(0, 20, 2, device=DEV)
+    n, start = ints([10] + [-1] * 5), ints([0] * 6)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(200_000_000)
+    if inside:
+        with torch.cuda.stream(side):
+            gpu.pi0_pages_compact(keep, n, start=start, stream=side)
+    else:
+        gpu.pi0_pages_compact(keep, n, start=start, stream=side)
+    where = keep.data_ptr()
+    del keep
+    other = torch.empty((6, big), dtype=torch.int32, device=DEV)
+    busy = not side.query()
+    assert busy and other.data_ptr() != where
+    side.synchronize()
+    cpu.compact([list(range(0, 20, 2))] * 6, [10] + [-1] * 5, [0] * 6)
+    gpu.pi0_pages_status()
+    same(gpu, cpu)
