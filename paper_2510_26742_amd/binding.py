@@ -545,13 +545,15 @@ def pi0_qk_norm_rope(pages: Pages, layer: int, q, k, v, row_start, max_rows: int
 
 
 def pi0_tree_attention(pages: Pages, layer: int, q, row_start, max_rows: int, *, mask=None, scale: Optional[float] = None, out=None, stream=None):
-    """q [n, heads, head_dim] of the cache's type; mask int32 [n, words] (bit j % 32 of word j / 32: sees token j of its sequence) or None
+    """q [n, heads, head_dim] of the cache's type; mask int32 [n, 1 or more words] (bit j % 32 of word j / 32: sees token j of its sequence) or None
     (all up to itself); scale None: head_dim ** -0.5.  Returns `out`, or a new tensor."""
     import torch
     n, d = q.shape[0], pages._c.head_dim
     _int32(row_start, "row_start", pages.n_seqs + 1)
     if mask is not None:
         _int32(mask, "mask", n, None)
+        if mask.shape[1] == 0:   # the library would take it for no mask
+            _refuse("mask: one word or more expected")
     handle, on = pages._on(stream, q, out, row_start, mask)
     with on:
         if out is None:

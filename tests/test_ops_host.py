@@ -260,3 +260,21 @@ def test_layers_that_one_launch_can_move(L):
         assert L.pi0_pages_compact(wide(**kw), None, FAKE, 1, FAKE, FAKE, 1 << 40, None) == binding.PI0_EINVAL
     # the grid of the largest that is taken: blocks of 128 elements, keys and values
     assert (1 << 29) // 128 * 2 * 256 + 2 * 256 * (1 << 16) < 1 << 32
+
+
+def cache_without_a_gpu(**kw):
+    """What the checks of arguments look at, of a cache whose tensors are on no GPU."""
+    p = object.__new__(binding.Pages)
+    p._c = good(**{**dict(n_seqs=2), **kw})
+    p._ref, p.n_seqs, p.device, p._index, p._streams = ctypes.byref(p._c), 2, torch.device("cuda:0"), 0, set()
+    return p
+
+
+def test_a_mask_of_no_words_is_not_no_mask(L):
+    """Rows that would see no drafted token at all are not taken for rows that see all up to themselves."""
+    p = cache_without_a_gpu()
+    p._on = lambda *a: pytest.fail("taken")
+    q, starts = torch.zeros((3, 8, 256), dtype=torch.bfloat16), torch.zeros(3, dtype=torch.int32)
+    with pytest.raises(binding.Pi0Error) as e:
+        binding.pi0_tree_attention(p, 0, q, starts, 2, mask=torch.zeros((3, 0), dtype=torch.int32))
+    assert e.value.code == binding.PI0_EINVAL
