@@ -166,7 +166,8 @@ int pi0_qk_norm_rope(const pi0_pages* pages, int layer, const pi0_rows* q, const
  *   q, out    n_rows rows of `heads` heads, a multiple of kv_heads; both of the cache's type; out may be q itself
  *   max_rows  most new tokens of a sequence, 1 .. 1024; n_seqs * kv_heads * ceil(max_rows * heads / kv_heads / 16) *
  *             (max_pages * page_tokens / 32 + 7) below 2^30
- *   d_mask    uint32 [n_rows][mask_words], or NULL (mask_words 0); bits behind the last word are clear
+ *   d_mask    uint32 [n_rows][mask_words], 1 .. 32 words, or NULL (mask_words 0); bits behind the last word are clear
+ *   scale     any number of magnitude below 2^127
  * Products on matrix cores with fp32 sums, softmax in fp32, its weights rounded to the cache's type in front of the second
  * product.  The workspace is scratch of this call: 16-byte aligned, pi0_tree_attention_workspace_bytes
  * of the same arguments (0: invalid arguments).  Errors: EINVAL, ENOMEM (workspace), EHIP.

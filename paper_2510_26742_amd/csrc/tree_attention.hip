@@ -801,7 +801,7 @@ size_t pi0_tree_attention_workspace_bytes(const pi0_pages* pages, int heads, int
 int pi0_tree_attention(const pi0_pages* pages, int layer, const pi0_rows* q, const pi0_rows* out, const int32_t* d_row_start, int n_rows,
                        int max_rows, const uint32_t* d_mask, int mask_words, float scale, void* d_workspace, size_t ws_bytes, void* hip_stream) {
   if (q == nullptr || d_row_start == nullptr || ((uintptr_t)d_row_start & 3) != 0 || !args_ok(pages, q->heads, n_rows, max_rows)) return PI0_EINVAL;
-  if (layer < 0 || layer >= pages->layers || !(scale - scale == 0.f)) return PI0_EINVAL;
+  if (layer < 0 || layer >= pages->layers || !(fabsf(scale) < 0x1p127f)) return PI0_EINVAL;   // (times log2(e) it is still a number)
   if (!rows_ok(q, 0, pages->head_dim, pages->dtype) || !rows_ok(out, q->heads, pages->head_dim, pages->dtype)) return PI0_EINVAL;
   if (mask_words < 0 || mask_words > 32 || (mask_words == 0) != (d_mask == nullptr) || ((uintptr_t)d_mask & 3) != 0) return PI0_EINVAL;
   if (d_workspace == nullptr || ((uintptr_t)d_workspace & 15) != 0) return PI0_EINVAL;

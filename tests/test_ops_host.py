@@ -278,3 +278,11 @@ def test_a_mask_of_no_words_is_not_no_mask(L):
     with pytest.raises(binding.Pi0Error) as e:
         binding.pi0_tree_attention(p, 0, q, starts, 2, mask=torch.zeros((3, 0), dtype=torch.int32))
     assert e.value.code == binding.PI0_EINVAL
+
+
+def test_a_scale_that_overflows(L):
+    """The kernel takes scale * log2(e): where that is infinite, scores of zero would become NaN."""
+    ref = ctypes.byref
+    need = L.pi0_tree_attention_workspace_bytes(ref(good()), 8, 3, 3)
+    for scale in (2.0 ** 127, -2.0 ** 127, 3e38, -3.4e38):
+        assert L.pi0_tree_attention(ref(good()), 0, ref(rows(8)), ref(rows(8)), FAKE, 3, 3, None, 0, scale, FAKE, need, None) == binding.PI0_EINVAL, scale
