@@ -407,7 +407,12 @@ def _rows(t, name: str, n_rows: int, heads: Optional[int], head_dim: int) -> Row
     if dtype is None or len(shape) != 3 or shape[0] != n_rows or heads not in (None, shape[1]) or shape[2] != head_dim or stride[2] != 1:
         _refuse(f"{name}: [{n_rows}, {heads or 'heads'}, {head_dim}] of a floating type expected")
     # (of a single row or head the stride says nothing)
-    return RowsC(t.data_ptr(), stride[0] if n_rows > 1 else max(stride[0], head_dim), stride[1] if shape[1] > 1 else head_dim, shape[1], dtype)
+    return RowsC(t.data_ptr(), stride[0] if n_rows > 1 else head_dim, stride[1] if shape[1] > 1 else head_dim, shape[1], dtype)
+
+
+def _strides(t):
+    """A cache's strides in front of head_dim; of a single layer, page or head the stride says nothing."""
+    return [s if n > 1 else 0 for s, n in zip(t.stride()[:4], t.shape)]
 
 
 class Pages:
@@ -417,7 +422,7 @@ class Pages:
 
     def __init__(self, k, v, table, length, refs):
         import torch
-        if k.dim() != 5 or k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype or k.stride(4) != 1 or _dtypes().get(k.dtype) is None:
+        if k.dim() != 5 or k.shape != v.shape or _strides(k) != _strides(v) or k.dtype != v.dtype or k.stride(4) != 1 or v.stride(4) != 1 or _dtypes().get(k.dtype) is None:
             _refuse("k, v: [layers, n_pages, page_tokens, kv_heads, head_dim] of one type and layout expected")
         layers, n_pages, page_tokens, kv_heads, head_dim = k.shape
         _int32(table, "table", None, None)
@@ -433,7 +438,7 @@ class Pages:
         self._streams = set()   # other streams that calls have run on
         self.n_seqs = int(table.shape[0])
         self._c = PagesC(k.data_ptr(), v.data_ptr(), table.data_ptr(), length.data_ptr(), refs.data_ptr(), self.status.data_ptr(),
-                         *k.stride()[:4], _dtypes()[k.dtype], layers, n_pages, page_tokens, kv_heads, head_dim, *table.shape)
+                         *_strides(k), _dtypes()[k.dtype], layers, n_pages, page_tokens, kv_heads, head_dim, *table.shape)
         self._ref = ctypes.byref(self._c)
         self._plan_bytes = int(lib().pi0_pages_workspace_bytes(self._ref))
         if self._plan_bytes == 0:

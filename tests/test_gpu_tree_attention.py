@@ -413,3 +413,18 @@ def test_in_place_where_blocks_have_many_units(d, dtype):
         binding.pi0_tree_attention(c.pages, c.layer, q, starts, c.most, mask=c.mask, out=q)
         assert torch.equal(q[mine].view(torch.int16), c.out[mine].view(torch.int16))
         assert torch.equal(q[:c.before], c.q[:c.before]) and torch.equal(q[mine.stop:], c.q[mine.stop:])
+
+
+def test_axes_of_one_with_any_stride():
+    """One token whose queries lie in a row of odd width, over one head, in one layer, whose axes have strides that say nothing."""
+    rng = np.random.default_rng(140)
+    k, v = (torch.from_numpy(rng.standard_normal((1, 4, 16, 64, 1))).to(DEV, torch.bfloat16).transpose(3, 4) for _ in range(2))
+    v = v.as_strided(v.shape, (7, 16 * 64, 64, 3, 1))
+    pages = binding.Pages(k, v, ints([[2, 0, 3, -1]]), ints([40]), ints([1, 0, 1, 1]))
+    q = torch.from_numpy(rng.standard_normal(8 * 64 + 3)).to(DEV, torch.bfloat16).as_strided((1, 8, 64), (515, 64, 1))
+    out = binding.pi0_tree_attention(pages, 0, q, ints([0, 1]), 1)
+    held = [f64(t[0, [2, 0, 3]].reshape(-1, 1, 64))[:41] for t in (k, v)]
+    want = paged.attention(f64(q), *held, np.ones((1, 41), dtype=bool), 0.125)
+    assert np.abs(f64(out) - want).max() <= 2.0 ** -7 * np.abs(held[1]).max()
+    binding.pi0_qk_norm_rope(pages, 0, q, q[:, :1], q[:, 1:2], ints([0, 1]), 1, rope_dim=0)
+    assert torch.equal(k[0, 3, 8, 0], q[0, 0]) and torch.equal(v[0, 3, 8, 0], q[0, 1])

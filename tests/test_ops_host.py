@@ -286,3 +286,19 @@ def test_a_scale_that_overflows(L):
     need = L.pi0_tree_attention_workspace_bytes(ref(good()), 8, 3, 3)
     for scale in (2.0 ** 127, -2.0 ** 127, 3e38, -3.4e38):
         assert L.pi0_tree_attention(ref(good()), 0, ref(rows(8)), ref(rows(8)), FAKE, 3, 3, None, 0, scale, FAKE, need, None) == binding.PI0_EINVAL, scale
+
+
+def test_strides_of_a_single_row_or_head_say_nothing(L):
+    """A token's queries out of a fused row of odd width, a head whose axis has stride 1."""
+    ref = ctypes.byref
+    fused = torch.zeros((5, 10 * 64 + 3), dtype=torch.bfloat16)
+    one = fused[2:3, :512].unflatten(1, (8, 64))
+    r = binding._rows(one, "q", 1, 8, 64)
+    assert r.row_stride % 8 == 0 and r.row_stride >= 64 and r.head_stride == 64 and r.d_x == one.data_ptr()
+    head = torch.zeros((3, 64, 1), dtype=torch.bfloat16).transpose(1, 2)
+    assert head.stride(1) == 1 and binding._rows(head, "q", 3, 1, 64).head_stride == 64
+    k = torch.zeros((2, 5, 16, 64, 1), dtype=torch.bfloat16).transpose(3, 4)
+    assert k.stride(3) == 1 and binding._strides(k) == [5 * 16 * 64, 16 * 64, 64, 0]
+    p = good(layers=2, n_pages=5, page_tokens=16, head_dim=64)
+    p.layer_stride, p.page_stride, p.token_stride, p.head_stride = binding._strides(k)
+    assert L.pi0_pages_workspace_bytes(ref(p)) > 0
