@@ -118,7 +118,8 @@ int pi0_pages_compact(const pi0_pages* pages, const int32_t* d_start, const int3
  * values of all layers into the sequence's pages, length[seq] = its tokens.  The pages must be there (pi0_pages_reserve on
  * the emptied sequence) and be the sequence's own.
  * Needs kv_heads 1, head_dim 256, PI0_BF16 and layers = llm_layers.  Failing on the device, nothing changed: PI0_ENOMEM
- * (too few pages), PI0_EINVAL (a page that others hold too).  Errors: EINVAL, ESTATE (no valid prefill), EHIP.
+ * (too few pages), PI0_EINVAL (a page that others hold too).  Errors: EINVAL, ESTATE (no valid prefill, or
+ * another device than that of pi0_load_weights is current), EHIP.
  */
 int pi0_pages_store(pi0_ctx* ctx, const pi0_pages* pages, int seq, void* hip_stream);
 
@@ -127,7 +128,7 @@ int pi0_pages_store(pi0_ctx* ctx, const pi0_pages* pages, int seq, void* hip_str
  * there; pi0_denoise (and the denoise half of the next pi0_stream_frame) then runs against them, its suffix at position
  * n_tokens.  Any number from one view's tokens up to max_views * tokens per view + max_prompt, for instance a prefix
  * stored earlier, or one with decoded tokens behind it.  Positions without a page are zero.
- * Errors: EINVAL (also: another geometry than pi0_pages_store takes), ESTATE (weights not loaded), EHIP.
+ * Errors: EINVAL (also: another geometry than pi0_pages_store takes), ESTATE (weights not loaded, or another device is current), EHIP.
  */
 int pi0_pages_load(pi0_ctx* ctx, const pi0_pages* pages, int seq, int n_tokens, void* hip_stream);
 

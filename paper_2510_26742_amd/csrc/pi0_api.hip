@@ -2248,6 +2248,11 @@ int pi0_stream_frame(pi0_ctx* c, const float* d_images, int n_views, const int32
 static bool pages_take_prefix(const pi0_ctx* c, const pi0_pages* p, int seq) {
   return pages_ok(p) && seq >= 0 && seq < p->n_seqs && p->kv_heads == 1 && p->head_dim == 256 && p->dtype == PI0_BF16 && p->layers == c->d.Ll;
 }
+// the ctx's cache lies on the device of its weights, pages and stream on the current one
+static bool on_its_device(const pi0_ctx* c) {
+  int dev = -1;
+  return hipGetDevice(&dev) == hipSuccess && dev == c->device;
+}
 // which prefix the ctx holds is known on the host: a call in a graph would go on with the one of its capture
 static hipError_t not_captured(hipStream_t s) {
   hipStreamCaptureStatus capturing = hipStreamCaptureStatusNone;
@@ -2257,7 +2262,7 @@ static hipError_t not_captured(hipStream_t s) {
 
 int pi0_pages_store(pi0_ctx* c, const pi0_pages* pages, int seq, void* hip_stream) {
   if (c == nullptr || !pages_take_prefix(c, pages, seq)) return PI0_EINVAL;
-  if (!c->loaded || c->cur_views == 0) return PI0_ESTATE;
+  if (!c->loaded || c->cur_views == 0 || !on_its_device(c)) return PI0_ESTATE;
   const WsLayout& w = c->wl;
   hipStream_t s = reinterpret_cast<hipStream_t>(hip_stream);
   hipError_t e = not_captured(s);
@@ -2270,7 +2275,7 @@ int pi0_pages_store(pi0_ctx* c, const pi0_pages* pages, int seq, void* hip_strea
 int pi0_pages_load(pi0_ctx* c, const pi0_pages* pages, int seq, int n_tokens, void* hip_stream) {
   if (c == nullptr || !pages_take_prefix(c, pages, seq)) return PI0_EINVAL;
   if (n_tokens < c->d.T || n_tokens > c->cfg.max_views * c->d.T + c->cfg.max_prompt) return PI0_EINVAL;
-  if (!c->loaded) return PI0_ESTATE;
+  if (!c->loaded || !on_its_device(c)) return PI0_ESTATE;
   const WsLayout& w = c->wl;
   hipStream_t s = reinterpret_cast<hipStream_t>(hip_stream);
   hipError_t e = not_captured(s);

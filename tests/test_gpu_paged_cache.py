@@ -218,3 +218,19 @@ def test_steps_of_drafting(heads, kv_heads, d, page, dtype):
         np.testing.assert_array_equal(bits(pages.k), plain.k)
         np.testing.assert_array_equal(bits(pages.v), plain.v)
     assert plain.length[0] > 40
+
+
+@pytest.mark.skipif(torch.cuda.device_count() < 2, reason="needs a second GPU: a cache on another one than the ctx's")
+def test_a_cache_on_another_device_than_the_ctx(model):
+    cfg, m, stream = model
+    images, ids, state, noise = inputs(cfg, 1, 0)
+    m.pi0_prefill(images, 1, None, 0, stream)
+    stream.synchronize()
+    far = lambda t: t.to("cuda:1")
+    near = empty(cfg.llm_layers, 6, 64, 1, 6)
+    pages = binding.Pages(*[far(t) for t in (near.k, near.v, near.table, near.length, near.refs)])
+    for call in (lambda: pages.pi0_pages_store(m, 0), lambda: pages.pi0_pages_load(m, 0, 256)):
+        with pytest.raises(binding.Pi0Error) as e:
+            call()
+        assert e.value.code == binding.PI0_ESTATE
+    assert torch.isfinite(denoise(cfg, m, stream, state, noise)).all()
