@@ -114,9 +114,10 @@ int pi0_pages_compact(const pi0_pages* pages, const int32_t* d_start, const int3
                       void* d_workspace, size_t ws_bytes, void* hip_stream);
 
 /*
- * The prefix that the last pi0_prefill / pi0_infer / pi0_pages_load left in ctx, as the contents of sequence seq: its keys (rotated) and
- * values of all layers into the sequence's pages, length[seq] = its tokens.  The pages must be there (pi0_pages_reserve on
- * the emptied sequence) and be the sequence's own.
+ * The prefix that the last pi0_prefill / pi0_infer / pi0_stream_frame / pi0_pages_load left in ctx, as the contents of sequence seq: its keys
+ * (rotated) and values of all layers into the sequence's pages, length[seq] = its tokens.  The pages must be there (pi0_pages_reserve on
+ * the emptied sequence) and be the sequence's own.  Store and load are ordered by their stream alone, as pi0_prefill is: between
+ * frames, and in front of the first, both belong on stream_prefill.
  * Needs kv_heads 1, head_dim 256, PI0_BF16 and layers = llm_layers.  Failing on the device, nothing changed: PI0_ENOMEM
  * (too few pages), PI0_EINVAL (a page that others hold too).  Errors: EINVAL, ESTATE (no valid prefill, or
  * another device than that of pi0_load_weights is current), EHIP.
@@ -125,8 +126,8 @@ int pi0_pages_store(pi0_ctx* ctx, const pi0_pages* pages, int seq, void* hip_str
 
 /*
  * The way back: the first n_tokens positions of sequence seq become the ctx's prefix, as if pi0_prefill had left them
- * there; pi0_denoise (and the denoise half of the next pi0_stream_frame) then runs against them, its suffix at position
- * n_tokens.  Any number from one view's tokens up to max_views * tokens per view + max_prompt, for instance a prefix
+ * there; pi0_denoise (and the denoise half of the next pi0_stream_frame, if the load was on its stream_prefill) then runs against them, its
+ * suffix at position n_tokens.  Any number from one view's tokens up to max_views * tokens per view + max_prompt, for instance a prefix
  * stored earlier, or one with decoded tokens behind it.  Positions without a page are zero.
  * Errors: EINVAL (also: another geometry than pi0_pages_store takes), ESTATE (weights not loaded, or another device is current), EHIP.
  */

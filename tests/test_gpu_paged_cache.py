@@ -234,3 +234,58 @@ def test_a_cache_on_another_device_than_the_ctx(model):
             call()
         assert e.value.code == binding.PI0_ESTATE
     assert torch.isfinite(denoise(cfg, m, stream, state, noise)).all()
+
+
+def test_load_and_store_between_frames(model):
+    """A prefix that was loaded, in front of the first frame of a ctx and between later ones, is what the next frame's denoise runs against, bit for
+    bit, also at lengths that no prefill leaves; what a frame's prefill left can be stored."""
+    cfg, m, stream = model
+    lengths = [300, 816, 544]
+    images, ids, _, _ = inputs(cfg, 3, 48)
+    m.pi0_prefill(images, 3, ids, 48, stream)
+    pages = empty(cfg.llm_layers, 230, 16, 5, 60)
+    pages.pi0_pages_reserve(ints([816, -1, -1, -1, -1]), stream=stream)
+    pages.pi0_pages_store(m, 0, stream=stream)
+    pages.pi0_pages_fork(ints([0, 0]), ints([1, 2]), stream=stream)
+    keep = np.zeros((5, 816), dtype=np.int64)
+    for s, n in ((0, 300), (2, 544)):
+        keep[s, :n] = np.sort(np.random.default_rng(n).permutation(816)[:n])
+    pages.pi0_pages_compact(ints(keep), ints([300, -1, 544, -1, -1]), start=ints([0] * 5), stream=stream)
+    frames = [inputs(cfg, v, p, seed=30 + i) for i, (v, p) in enumerate([(1, 0), (2, 9), (1, 5), (3, 0)])]
+    shapes = [(1, 0), (2, 9), (1, 5), (3, 0)]
+    # frame i's denoise: against a loaded prefix (0, 1, 2), the third's against the frame before
+    want = []
+    for i, n in enumerate([*lengths, None]):
+        if n is not None:
+            pages.pi0_pages_load(m, i, n, stream=stream)
+        else:
+            m.pi0_prefill(frames[2][0], *shapes[2][:1], frames[2][1], shapes[2][1], stream)
+        want.append(denoise(cfg, m, stream, *frames[i][2:]))
+    P = 3 * 256
+    pages.pi0_pages_reserve(ints([-1, -1, -1, P, P]), stream=stream)
+    m.pi0_prefill(frames[3][0], 3, None, 0, stream)
+    pages.pi0_pages_store(m, 3, stream=stream)
+    pages.pi0_pages_status(stream)
+
+    sp, sd = torch.cuda.Stream(), torch.cuda.Stream()
+    m2 = binding.Pi0(cfg)
+    m2.pi0_load_weights(torch.from_numpy(synth.make_weights(cfg, seed=0).view(np.int16)).to(DEV), sp)
+    torch.cuda.synchronize()
+    for again in range(2):              # the ctx's first frame, and with all of its graphs there
+        got = [torch.full_like(want[0], float("nan")) for _ in want]
+        torch.cuda.synchronize()
+        for i, (f, (views, prompt)) in enumerate(zip(frames, shapes)):
+            print("[gpu] frame", again, i, flush=True)
+            if i < 3:
+                pages.pi0_pages_load(m2, i, lengths[i], stream=sp)
+            m2.pi0_stream_frame(f[0], views, f[1], prompt, f[2], f[3], got[i], sp, sd)
+        pages.pi0_pages_store(m2, 4, stream=sp)
+        sp.synchronize()
+        sd.synchronize()
+        m2.pi0_device_status(sd)
+        for a, b in zip(got, want):
+            assert torch.equal(a, b)
+        pages.pi0_pages_status(sp)
+        a, b = (torch.stack([t[:, pages.table[s, :P // 16].long()] for t in (pages.k, pages.v)]) for s in (3, 4))
+        assert torch.equal(a.view(torch.int16), b.view(torch.int16)) and pages.length.tolist()[3:] == [P, P]
+    m2.close()
