@@ -163,18 +163,8 @@ template <int CTRL, int ROWS = 0xf, class V>
 __device__ __forceinline__ V dpp(V v) {
   return __builtin_bit_cast(V, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, ROWS, 0xf, false));
 }
-// sums over a wave's lanes, in every lane
-__device__ __forceinline__ float wave_sum(float v) {
-  v += dpp<0x111>(v);   // lanes 1, 2, 4, 8 below, inside rows of 16; then the rows' last lanes to the rows behind
-  v += dpp<0x112>(v);
-  v += dpp<0x114>(v);
-  v += dpp<0x118>(v);
-  v += dpp<0x142, 0xa>(v);
-  v += dpp<0x143, 0xc>(v);
-  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
-}
 __device__ __forceinline__ int wave_prefix(int v) {   // sum over the lanes up to this one
-  v += dpp<0x111>(v);
+  v += dpp<0x111>(v);   // lanes 1, 2, 4, 8 below, inside rows of 16; then the rows' last lanes to the rows behind
   v += dpp<0x112>(v);
   v += dpp<0x114>(v);
   v += dpp<0x118>(v);
