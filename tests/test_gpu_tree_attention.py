@@ -428,3 +428,37 @@ def test_axes_of_one_with_any_stride():
     assert np.abs(f64(out) - want).max() <= 2.0 ** -7 * np.abs(held[1]).max()
     binding.pi0_qk_norm_rope(pages, 0, q, q[:, :1], q[:, 1:2], ints([0, 1]), 1, rope_dim=0)
     assert torch.equal(k[0, 3, 8, 0], q[0, 0]) and torch.equal(v[0, 3, 8, 0], q[0, 1])
+
+
+@pytest.mark.parametrize("d,dtype", [(256, "bf16"), (128, "f16"), (64, "bf16")])
+def test_missing_pages_where_rows_are_many(d, dtype):
+    """Tiles of 128 rows, whose scores run a granule ahead: halves of a unit's first, middle and last granules are on no page, whole granules, and
+    a sequence's every page."""
+    c = Case(150, [100, 64, 0, 333, 40], [20, 20, 33, 17, 20], 8, 1, d, 16, dtype, kind="random")
+    gone = [[0, 5, 7], [0, 1, 4], [0, 2], [1, 2, 3, 10, 21], [0, 1, 2, 3]]
+    for s, idx in enumerate(gone):
+        for i in idx:
+            c.pages.table[s, i] = [-1, c.pages.k.shape[1], 1 << 30][i % 3]
+
+    def seen(s):
+        x = c.seen(s).copy()
+        for i in gone[s]:
+            x[:, 16 * i:16 * i + 16] = False
+        return x
+    c.run()
+    c.check(seen=seen)
+
+
+def test_as_many_rows_as_there_can_be():
+    """1024 tokens of 1024 heads over one: 2^20 rows.  Queries of zero make a token's result the mean of the values that it sees, here half its number -
+    a different one for each token, and fp16 tells them apart."""
+    n, d = 1024, 64
+    k = torch.zeros((1, 65, 16, 1, d), dtype=torch.float16, device=DEV)
+    v = torch.arange(65 * 16, device=DEV).reshape(1, 65, 16, 1, 1).expand(1, 65, 16, 1, d).to(torch.float16).contiguous()
+    pages = binding.Pages(k, v, ints([np.arange(65)]), ints([0]), ints(np.ones(65)))
+    q = torch.zeros((n, n, d), dtype=torch.float16, device=DEV)
+    out = torch.full_like(q, float("nan"))
+    binding.pi0_tree_attention(pages, 0, q, ints([0, n]), n, out=out)
+    # sums of whole numbers, times a power of two, are exact in 32 bits; the quotient is off by 2^-14 at most, and halves below 512 are numbers of fp16
+    want = (torch.arange(n, device=DEV, dtype=torch.float32) / 2).to(torch.float16)
+    assert torch.equal(out, want[:, None, None].expand(n, n, d))

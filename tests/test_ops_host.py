@@ -302,3 +302,15 @@ def test_strides_of_a_single_row_or_head_say_nothing(L):
     p = good(layers=2, n_pages=5, page_tokens=16, head_dim=64)
     p.layer_stride, p.page_stride, p.token_stride, p.head_stride = binding._strides(k)
     assert L.pi0_pages_workspace_bytes(ref(p)) > 0
+
+
+def test_the_reciprocal_finds_a_rows_token():
+    """Attention finds row r's token as (r + 1/2) * reciprocal(group) in fp32, cut off.  At the first and last row of every token, for every group up to
+    1024 and 1024 tokens, with a reciprocal one step to either side of the rounded one, as far off as the hardware's may be."""
+    token = np.arange(1024, dtype=np.int64)
+    for group in range(1, 1025):
+        near = np.float32(1.0) / np.float32(group)
+        for reciprocal in (np.nextafter(near, np.float32(0)), near, np.nextafter(near, np.float32(2))):
+            for row in (token * group, token * group + group - 1):
+                found = ((row.astype(np.float32) + np.float32(0.5)) * np.float32(reciprocal)).astype(np.int64)
+                assert np.array_equal(found, token), group
