@@ -335,3 +335,27 @@ def test_what_a_call_was_given_stays_until_it_has_run(inside):
     cpu.compact([list(range(0, 20, 2))] * 6, [10] + [-1] * 5, [0] * 6)
     gpu.pi0_pages_status()
     same(gpu, cpu)
+
+
+def test_free_pages_far_behind_others():
+    """50 000 pages that others hold in front of the first free ones, which lie one by one and in runs across the reads of a search."""
+    gpu, cpu = make(12, layers=1, n_pages=53_000, page=16, kv_heads=1, head_dim=64, n_seqs=3, max_pages=1200)
+    taken = np.ones(53_000, dtype=np.int64)
+    free = np.concatenate([[3, 1023, 1024], [50_000, 50_175, 50_176], np.arange(51_190, 51_700), [52_999], np.arange(52_000, 52_990)])
+    taken[free] = 0
+    gpu.refs.copy_(ints(taken))
+    cpu.refs = taken.tolist()
+    for extra in ([20, 50, -1], [16 * 5, -1, 16 * 700], [16 * 200, 3, 0]):
+        gpu.pi0_pages_reserve(ints(extra))
+        cpu.reserve(extra)
+        gpu.pi0_pages_compact(ints([[0, 1, 2, 3]] * 3), ints([min(e, 4) for e in extra]))
+        cpu.compact([[0, 1, 2, 3]] * 3, [min(e, 4) for e in extra])
+        gpu.pi0_pages_status()
+        same(gpu, cpu, str(extra))
+    gpu.pi0_pages_reserve(ints([16 * 600, 16 * 600, 16 * 600]))
+    with pytest.raises(paged.Refused):
+        cpu.reserve([16 * 600] * 3)
+    with pytest.raises(binding.Pi0Error) as e:
+        gpu.pi0_pages_status()
+    assert e.value.code == binding.PI0_ENOMEM
+    same(gpu, cpu, "refused")
