@@ -64,7 +64,7 @@ typedef struct pi0_pages {
  * Rows of heads: element e of head h of row r at d_x[r * row_stride + h * head_stride + e], strides in elements.
  * The new tokens of all sequences lie behind each other, those of sequence s in rows row_start[s] .. row_start[s + 1] - 1
  * (d_row_start int32 [n_seqs + 1], ascending); at most max_rows of a sequence are taken.  Rows that belong to no sequence, or
- * lie outside [0, n_rows), are neither read nor written.
+ * lie outside [0, n_rows), are neither read nor written.  n_rows is 1 .. 2^24, max_rows 1 .. n_rows: a call without a new token is none.
  */
 typedef struct pi0_rows {
   void* d_x;             /* 16-byte aligned                                                           */
@@ -88,7 +88,7 @@ size_t pi0_pages_workspace_bytes(const pi0_pages* pages);
 int pi0_pages_reserve(const pi0_pages* pages, const int32_t* d_extra, void* d_workspace, size_t ws_bytes, void* hip_stream);
 
 /*
- * Sequence d_dst[i] becomes a continuation of sequence d_src[i], i < n (int32 [n], device; n <= n_seqs): it holds the
+ * Sequence d_dst[i] becomes a continuation of sequence d_src[i], i < n (int32 [n], device; 1 <= n <= n_seqs): it holds the
  * same pages up to the committed length and lets go of those it held.  Nothing is copied before one of the two is
  * written to (see pi0_pages_reserve).
  * Failing on the device, nothing changed: PI0_EINVAL (an index outside [0, n_seqs), a dst that occurs twice or is a src
@@ -166,7 +166,7 @@ int pi0_qk_norm_rope(const pi0_pages* pages, int layer, const pi0_rows* q, const
  *     out = sum_j softmax_j(scale * q . k_j) v_j        over what the token sees; 0 if that is nothing
  * What a token does not see does not reach it, whatever is stored there (a NaN, an unwritten page).
  *   q, out    n_rows rows of `heads` heads, a multiple of kv_heads; both of the cache's type; out may be q itself
- *   max_rows  most new tokens of a sequence, 1 .. 1024; n_seqs * kv_heads * ceil(max_rows * heads / kv_heads / 16) *
+ *   max_rows  most new tokens of a sequence, 1024 at most; n_seqs * kv_heads * ceil(max_rows * heads / kv_heads / 16) *
  *             (max_pages * page_tokens / 32 + 7) below 2^30
  *   d_mask    uint32 [n_rows][mask_words], 1 .. 32 words, or NULL (mask_words 0); bits behind the last word are clear
  *   scale     any number of magnitude below 2^127

@@ -8,10 +8,12 @@
 // maxima need two exchanges between the quarters of a wave.  V^T is read out of row-major tiles with the transposing LDS
 // load (4 keys x 16 d per 16 lanes).  A wave has R times 16 rows: what it reads of K and V out of LDS serves all of them.  R = 1 where
 // the cache's own bytes are what the time goes to, 2 where rows are many.
-// What bounds it: few rows the reads of the cache (64 x 1 token, 8 heads over 1 of 256, up to 8192 keys: 277 MB in 43.6 us, 6.4 TB/s);
-// many rows the issue of instructions, of which a wave that is alone on its SIMD has one per 4 cycles (8 x 64 nodes over 16384: 25.8
-// GFLOP in 48 us, 540 TFLOP/s; a granule's 64 products per wave could end in 1024 cycles, but stand among 350 instructions), which is why the loop does nothing that
-// can be done in front of it.
+// What bounds it: few rows the reads of the cache (64 x 1 token, 8 heads over 1 of 256, up to 8192 keys: 277 MB in 43.4 us, 6.4 TB/s);
+// many rows what a wave that is alone on its SIMD does one after the other (8 x 64 nodes over 16384: 25.8 GFLOP in 47.4 us, 545 TFLOP/s).  A
+// granule takes it 2370 cycles: scores with weights and requests beside them 1070, sums with maxima 790, the barrier and the looks at what is to be cleaned,
+// hidden and rescaled the rest.  Its 64 products could end in 1024 (the matrix cores are busy 30 % of the kernel's time); its reads of shared memory
+// take 1150 (without conflicts 31 cycles per 16 bytes a lane, 21 per transposing read), its 350 instructions 1400 to issue.  28 granules are 66 of a
+// wave's 87 thousand cycles, the beginning and partial results the others.
 // Tiles come straight into LDS, 16 bytes per lane; the pieces of a row are permuted by its key (on the global side: a lane
 // may fetch any piece) so that neither product's reads collide in the banks.
 #include "pages_common.h"
@@ -483,6 +485,9 @@ __global__ __launch_bounds__(64 * RW, D < 256 || R == 1 ? 2 : 1) void tree_atten
         }
       }
     };
+    // Weights are rounded to the cache's type: the second product takes 16-bit operands, 32-bit ones have a sixteenth of the rate.  The
+    // distance of results from 64 bits, norm over norm, is 2.3e-3 with it and 1.7e-3 by their own last rounding alone (8 x 64 nodes over 16384, bf16), 2.4e-4
+    // and 2.1e-4 (16 x 33 over 3001, fp16).
     // (The empty assembly holds what is made beside products there: the compiler moves it behind the next branch otherwise.)
     unsigned pw[R][4];
     auto weigh = [&](const f32x8 (&s)[R], int pair) {   // two scores of this lane, of 4 R
@@ -729,7 +734,8 @@ Space space_of(const pi0_pages& p, int rows) {
 
 // f(R): 64 rows per tile, or 128 where there are more than that of enough sequences and heads (measured with 64 and with 128: 8 x 64 nodes
 // with 8 heads over 1 of 256 and 16384 keys 61.8 and 57.3 us, 16 x 33 with 32 over 8 of 128 and 4096 51.5 and 44.8; 1 x 64 over 2048
-// 20.8 and 23.4, 16 x 16, that is 128 rows, over 2048 20.2 and 23.3).
+// 20.8 and 23.4, 16 x 16, that is 128 rows, over 2048 20.2 and 23.3).  192 rows per tile fit the registers of heads of 256 (242 + 228) and are as fast
+// for 8 x 64, and spill for heads of 128.
 template <class F>
 auto with_rows(int rows, int heads, F f) {
   if (rows > 128 && heads >= 4) return f(std::integral_constant<int, 2>());
