@@ -359,3 +359,28 @@ def test_free_pages_far_behind_others():
         gpu.pi0_pages_status()
     assert e.value.code == binding.PI0_ENOMEM
     same(gpu, cpu, "refused")
+
+
+def test_as_many_sequences_as_there_can_be():
+    """1024 sequences in every operation, half of them continuations of the other half, shared pages replaced for all at once."""
+    gpu, cpu = make(13, layers=1, n_pages=5000, page=16, kv_heads=1, head_dim=64, n_seqs=1024, max_pages=4)
+    rng = np.random.default_rng(14)
+    grow(gpu, cpu, [int(x) for x in rng.integers(0, 40, 512)] + [0] * 512)
+    src, dst = [int(x) for x in rng.integers(0, 512, 512)], [int(x) for x in 512 + rng.permutation(512)]
+    gpu.pi0_pages_fork(ints(src), ints(dst))
+    cpu.fork(src, dst)
+    same(gpu, cpu, "forked")
+    extra = [int(x) for x in rng.integers(-1, 17, 1024)]
+    gpu.pi0_pages_reserve(ints(extra))
+    cpu.reserve(extra)
+    same(gpu, cpu, "reserved")
+    start = [int(rng.integers(0, n + 1)) for n in cpu.length]
+    rows = [np.flatnonzero(rng.random(len(t) * 16 - s) < 0.6) for t, s in zip(cpu.table, start)]
+    keep, n = np.zeros((1024, 64), dtype=np.int64), []
+    for s, r in enumerate(rows):
+        keep[s, :len(r)] = r
+        n.append(len(r) if s % 9 else -1)
+    gpu.pi0_pages_compact(ints(keep), ints(n), start=ints(start))
+    cpu.compact(keep, n, start)
+    gpu.pi0_pages_status()
+    same(gpu, cpu, "compacted")
